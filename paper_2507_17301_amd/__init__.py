@@ -5,4 +5,4 @@
 synthetic layer tables and seeded generators.  Importing the package loads
 nothing native; the library is opened on first use and its absence is an error.
 """
-__all__ = ["binding", "workloads", "build"]
+__all__ = ["binding", "workloads", "build", "network", "feedforward"]

@@ -1,6 +1,6 @@
 """ctypes binding of libnmconv.so -- argument marshalling only.
 
-Same names as the C ABI in ``include/nm_conv.h``.  Tensors are torch tensors
+Same names as the C ABI in ``include/nm_conv.h`` and ``include/nm_q8.h``.  Tensors are torch tensors
 used purely as device buffers (``data_ptr()``) and for the current stream; all
 arithmetic happens inside the library's kernels.  There is no fallback: if the
 library is missing or a call fails, an exception is raised.
@@ -14,7 +14,8 @@ from typing import Optional, Tuple
 
 import numpy as np
 
-NM_F32, NM_BF16, NM_F8E4M3 = 0, 1, 2
+NM_F32, NM_BF16, NM_F8E4M3, NM_I8 = 0, 1, 2, 3
+NM_Q8_MAX_WIDTH = 65536
 NM_OK = 0
 NM_ERR_ARG, NM_ERR_SHAPE, NM_ERR_UNSUPPORTED, NM_ERR_ALLOC, NM_ERR_HIP, NM_ERR_IO = -1, -2, -3, -4, -5, -6
 _STATUS = {0: "NM_OK", -1: "NM_ERR_ARG", -2: "NM_ERR_SHAPE", -3: "NM_ERR_UNSUPPORTED",
@@ -74,12 +75,23 @@ def lib():
         L.nm_cache_load.argtypes = [ctypes.c_char_p]
         L.nm_force_variant.argtypes = [ci]
         L.nm_variant_legal.argtypes = [ci, vp, ci, ci]
+        i64, st = ctypes.c_int64, ctypes.c_size_t
+        L.nm_quantize_q8.argtypes = [vp, ci, i64, ci, i64, vp, i64, vp, vp]
+        L.nm_dequantize_q8.argtypes = [vp, i64, vp, i64, ci, vp, ci, i64, vp]
+        L.nm_rmsnorm_q8.argtypes = [vp, ci, i64, ci, i64, vp, i64, vp, cf, vp, i64, vp, i64, vp, vp]
+        L.nm_q8_pack.argtypes = [vp, ci, vp, ci, ci, i64, ci, vp, ctypes.POINTER(vp)]
+        L.nm_q8_free.argtypes = [vp]
+        L.nm_q8_dims.argtypes = [vp, pi, pi, pi]
+        L.nm_q8_export.argtypes = [vp, vp, vp]
+        L.nm_linear_q8.argtypes = [vp, i64, ci, i64, vp, vp, vp, vp, i64, vp, ci, i64, vp, st, vp]
+        L.nm_linear_q8_workspace.argtypes = [vp, i64, i64, vp, ctypes.POINTER(st)]
         for name in ("nm_prune", "nm_packed_free", "nm_packed_dims", "nm_packed_indices",
                      "nm_packed_values", "nm_packed_mask", "nm_packed_scale", "nm_conv2d", "nm_conv2d_res", "nm_conv2d_static", "nm_conv2d_args",
                      "nm_maxpool2d",
                      "nm_avgpool_global", "nm_im2col", "nm_stream_floor", "nm_autotune",
                      "nm_cache_save", "nm_cache_load", "nm_cache_clear", "nm_cache_size", "nm_workspace_free",
-                     "nm_force_variant", "nm_variant_legal"):
+                     "nm_force_variant", "nm_variant_legal", "nm_quantize_q8", "nm_dequantize_q8", "nm_rmsnorm_q8",
+                     "nm_q8_pack", "nm_q8_free", "nm_q8_dims", "nm_q8_export", "nm_linear_q8", "nm_linear_q8_workspace"):
             getattr(L, name).restype = ci
         _lib = L
     return _lib
@@ -398,3 +410,168 @@ def nm_force_variant(v: int):
 
 def nm_variant_legal(v: int, wp: Packed, x_dtype: int = NM_F32, y_dtype: int = NM_F32) -> bool:
     return _check(lib().nm_variant_legal(v, wp.handle, x_dtype, y_dtype)) == 1
+
+
+# ---------------------------------------------------------------- 8-bit feed-forward operators (nm_q8.h)
+def _rows_of(t, name: str):
+    """(rows, width, row stride) of a device tensor whose last axis is the row: two axes with any row stride, or any
+    number of them contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    shape = t.shape
+    if len(shape) == 2:
+        rows, width = shape
+        ld, inner = t.stride()
+        if inner != 1 and width > 1:
+            raise ValueError(f"the values of a row of {name} must be adjacent")
+        return rows, width, ld if rows > 1 else width
+    if len(shape) < 1 or not t.is_contiguous():
+        raise ValueError(f"{name} must be rows: two axes, or contiguous")
+    width = shape[-1]
+    return (t.numel() // width if width else 0), width, width
+
+
+def _q8_out(t, name: str, shape, dtype, like):
+    import torch
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if t.shape != shape or t.dtype != dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {like.device}")
+    return t
+
+
+def _q8_vector(t, name: str, n: int, like):
+    """Pointer of a contiguous fp32 vector of n values on the device of `like` (0 for None)."""
+    import torch
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or t.numel() != n or t.get_device() != like.get_device() or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous fp32 tensor of {n} values on {like.device}")
+    return t.data_ptr()
+
+
+def nm_quantize_q8(x, q=None, scales=None, stream=None):
+    """Rows of x (fp32 or bf16, the last axis) rounded to 8 bits: (q int8 like x, scales fp32 [rows...]) with x ~ q * scales."""
+    import torch
+    rows, width, ld = _rows_of(x, "x")
+    q = _q8_out(q, "q", x.shape, torch.int8, x)
+    scales = _q8_out(scales, "scales", x.shape[:-1], torch.float32, x)
+    rc = (_lib or lib()).nm_quantize_q8(x.data_ptr(), _dtype_code(x), rows, width, ld, q.data_ptr(), _rows_of(q, "q")[2],
+                                        _q8_vector(scales, "scales", rows, x), _stream_ptr(stream))
+    if rc < 0:
+        _check(rc)
+    return q, scales
+
+
+def nm_dequantize_q8(q, scales, dtype=None, y=None, stream=None):
+    """The values that 8-bit rows stand for, q * scales, in fp32 or bf16 (`dtype`; default fp32 or y's)."""
+    import torch
+    rows, width, ld = _rows_of(q, "q")
+    if q.dtype != torch.int8:
+        raise TypeError(f"q must be int8, not {q.dtype}")
+    y = _q8_out(y, "y", q.shape, dtype or (torch.float32 if y is None else y.dtype), q)
+    rc = (_lib or lib()).nm_dequantize_q8(q.data_ptr(), ld, _q8_vector(scales, "scales", rows, q), rows, width, y.data_ptr(),
+                                          _dtype_code(y), _rows_of(y, "y")[2], _stream_ptr(stream))
+    if rc < 0:
+        _check(rc)
+    return y
+
+
+def nm_rmsnorm_q8(x, gamma=None, residual=None, eps: float = 1e-6, q=None, scales=None, residual_out=None, stream=None):
+    """h = x + residual; rows of gamma * h / sqrt(mean(h^2) + eps) rounded to 8 bits.  Returns (q, scales, h rounded to x's
+    dtype); the last is None without a residual unless residual_out is given.  residual_out may be x or residual."""
+    import torch
+    rows, width, ld = _rows_of(x, "x")
+    ldr = rptr = ldo = optr = 0
+    if residual is not None:
+        if residual.shape != x.shape or residual.dtype != x.dtype or residual.get_device() != x.get_device():
+            raise ValueError("residual must be shaped and typed like x")
+        ldr, rptr = _rows_of(residual, "residual")[2], residual.data_ptr()
+        if residual_out is None:
+            residual_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if residual_out is not None:
+        residual_out = _q8_out(residual_out, "residual_out", x.shape, x.dtype, x)
+        ldo, optr = _rows_of(residual_out, "residual_out")[2], residual_out.data_ptr()
+    q = _q8_out(q, "q", x.shape, torch.int8, x)
+    scales = _q8_out(scales, "scales", x.shape[:-1], torch.float32, x)
+    rc = (_lib or lib()).nm_rmsnorm_q8(x.data_ptr(), _dtype_code(x), rows, width, ld, rptr, ldr, _q8_vector(gamma, "gamma", width, x),
+                                       eps, optr, ldo, q.data_ptr(), _rows_of(q, "q")[2], _q8_vector(scales, "scales", rows, x),
+                                       _stream_ptr(stream))
+    if rc < 0:
+        _check(rc)
+    return q, scales, residual_out
+
+
+class Q8Weights:
+    """Owner of an nm_q8_t handle: [channels, width] weights in 8 bits."""
+
+    def __init__(self, handle, channels: int, width: int, gated: bool):
+        self.handle = handle
+        self.channels, self.width, self.gated = channels, width, gated
+        self.outs = channels // 2 if gated else channels
+
+    def free(self):
+        """Release the handle now (idempotent)."""
+        h, self.handle = getattr(self, "handle", None), None
+        if h and _lib is not None:
+            _lib.nm_q8_free(h)
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def nm_q8_pack(w, scales=None, gated: bool = False, stream=None) -> Q8Weights:
+    """Weights [channels, width] on the device: int8 with fp32 scales [channels], or fp32 / bf16, which are rounded here
+    (a scale for each channel).  gated: the first half of the channels gates the second."""
+    import torch
+    if w.dim() != 2:
+        raise ValueError("w must have two axes")
+    channels, width, ld = _rows_of(w, "w")
+    sptr = _q8_vector(scales, "scales", channels, w)
+    code = NM_I8 if w.dtype == torch.int8 else _dtype_code(w)
+    h = ctypes.c_void_p()
+    _check(lib().nm_q8_pack(w.data_ptr(), code, sptr, channels, width, ld, int(bool(gated)), _stream_ptr(stream), ctypes.byref(h)))
+    return Q8Weights(h, channels, width, bool(gated))
+
+
+def nm_q8_export(w: Q8Weights):
+    """(int8 [channels, width], fp32 scales [channels]) as numpy arrays."""
+    a, s = np.empty((w.channels, w.width), dtype=np.int8), np.empty(w.channels, dtype=np.float32)
+    _check(lib().nm_q8_export(w.handle, a.ctypes.data, s.ctypes.data))
+    return a, s
+
+
+def nm_linear_q8(q, scales, w: Q8Weights, bias=None, residual=None, dtype=None, y=None, stream=None):
+    """8-bit rows times 8-bit weights: (q @ w.T) * scales * channel scales + bias + residual, or the gated form
+    silu(gate) * up.  y: [..., channels] (gated: half of them) in bf16 (default) or fp32; residual is typed and shaped
+    like y and may be y."""
+    import torch
+    rows, width, ld = _rows_of(q, "q")
+    if q.dtype != torch.int8:
+        raise TypeError(f"q must be int8, not {q.dtype}")
+    L = _lib or lib()
+    y = _q8_out(y, "y", q.shape[:-1] + (w.outs,), dtype or (torch.bfloat16 if y is None else y.dtype), q)
+    ldr = rptr = 0
+    if residual is not None:
+        if residual.shape != y.shape or residual.dtype != y.dtype or residual.get_device() != y.get_device():
+            raise ValueError("residual must be shaped and typed like the output")
+        ldr, rptr = _rows_of(residual, "residual")[2], residual.data_ptr()
+    need = ctypes.c_size_t(0)
+    rc = L.nm_linear_q8_workspace(q.data_ptr(), rows, ld, w.handle, ctypes.byref(need))
+    if rc < 0:
+        _check(rc)
+    ws = wptr = None
+    if need.value:
+        ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        wptr = ws.data_ptr()
+        if stream is not None:
+            ws.record_stream(stream)
+    rc = L.nm_linear_q8(q.data_ptr(), rows, width, ld, _q8_vector(scales, "scales", rows, q), w.handle,
+                        _q8_vector(bias, "bias", w.channels, q), rptr, ldr, y.data_ptr(), _dtype_code(y), _rows_of(y, "y")[2],
+                        wptr, need.value, _stream_ptr(stream))
+    if rc < 0:
+        _check(rc)
+    return y

@@ -150,7 +150,8 @@ def _shapes_wave():
 
 def _jobs():
     jobs = []
-    for src in ("nm_api.hip", "nm_prune_kernels.hip", "nm_pool_kernels.hip", "nm_conv_registry.hip", "nm_scratch.hip"):
+    for src in ("nm_api.hip", "nm_prune_kernels.hip", "nm_pool_kernels.hip", "nm_conv_registry.hip", "nm_scratch.hip",
+                "nm_q8_api.hip", "nm_q8_rows.hip", "nm_q8_linear.hip"):
         jobs.append((os.path.join(CSRC, src), os.path.join(OBJDIR, src.replace(".hip", ".o")), []))
     inst = os.path.join(CSRC, "nm_conv_inst.hip")
     for nb, wp, nj in _shapes():
@@ -217,9 +218,9 @@ def _jobs():
     return jobs
 
 
-def _newest_header():
-    hs = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    hs += [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE) if f.endswith(".h")]
+def _newest_header(q8=False):
+    """Time of the last change to a header; the headers of the 8-bit operators (nm_q8*) count for their own sources only."""
+    hs = [os.path.join(d, f) for d in (CSRC, INCLUDE) for f in os.listdir(d) if f.endswith(".h") and (q8 or not f.startswith("nm_q8"))]
     return max(os.path.getmtime(h) for h in hs)
 
 
@@ -242,10 +243,10 @@ def build(jobs: int = 8, force: bool = True) -> str:
     """Compile every translation unit and link libnmconv.so.  With force=False
     only out-of-date objects are rebuilt."""
     os.makedirs(OBJDIR, exist_ok=True)
-    hdr_time = _newest_header()
+    hdr_time = {q8: _newest_header(q8) for q8 in (False, True)}
     todo = _jobs()
     with ThreadPoolExecutor(max_workers=max(1, jobs)) as ex:
-        objs = list(ex.map(lambda j: _compile(j, force, hdr_time), todo))
+        objs = list(ex.map(lambda j: _compile(j, force, hdr_time[os.path.basename(j[0]).startswith("nm_q8")]), todo))
     cmd = [HIPCC, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:

@@ -1,0 +1,234 @@
+// Row operators in 8 bits: residual addition + root-mean-square norm + rounding, rounding alone, reading back.
+//
+//   h = x + r;  v = gamma * h / sqrt(mean(h^2) + eps);  s = max|v| / 127;  q = rint(v * 127 / max|v|)
+//
+// Bound by HBM: a value is read once (twice with a residual), kept in registers over both reductions (sum of
+// squares, largest magnitude), and written once.  NT threads share a row, 8 adjacent values a thread at a time,
+// so that a wavefront reads 1 KiB (bf16) or 2 KiB (fp32) of adjacent bytes an instruction and writes 512 bytes
+// of q.  One wavefront a row up to 1024 values (no barrier), 256 threads up to 16384, 1024 beyond.
+// Rows of odd widths and strides run the same code (global memory takes a 16-byte access at any address); only what a width leaves past its last group of 8 is
+// taken value by value, one value a thread.
+#include "nm_q8_device.h"
+
+namespace nm {
+namespace {
+
+struct RowArgs {
+    const char* x;
+    const char* res;
+    const float* gamma;
+    char* out;
+    int8_t* q;
+    float* scales;
+    int64_t rows, ldx, ldr, ldo, ldq;
+    int width;
+    float eps;
+};
+
+// Sum (or largest) over the NT threads of a row; `part` holds one slot for each wavefront of the row.
+template <int NT>
+__device__ inline float row_sum(float v, float* part)
+{
+    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
+    if constexpr (NT > 64) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+        for (int i = 0; i < NT / 64; ++i) v += part[i];
+    }
+    return v;
+}
+template <int NT>
+__device__ inline unsigned row_max(unsigned v, unsigned* part)
+{
+    for (int m = 1; m < 64; m <<= 1) v = max(v, (unsigned)__shfl_xor((int)v, m));
+    if constexpr (NT > 64) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        for (int i = 0; i < NT / 64; ++i) v = max(v, part[i]);
+    }
+    return v;
+}
+
+template <bool BF16, int NT, int VPT, bool NORM>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
+{
+    constexpr int ES = Elem<BF16>::kBytes, BLOCK = NT < 256 ? 256 : NT, RPB = BLOCK / NT;
+    __shared__ float psum[NT / 64];
+    __shared__ unsigned pmax[NT / 64];
+    const int t = threadIdx.x % NT;
+    const int whole = p.width & ~7, over = p.width & 7;   // the values past the last group of 8: one each for the first threads
+    // (with several rows a workgroup there is no barrier, and its wavefronts may leave the loop apart)
+    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT; row < p.rows; row += (int64_t)gridDim.x * RPB) {
+        const char* px = p.x + row * p.ldx * ES;
+        const char* pr = NORM && p.res ? p.res + row * p.ldr * ES : nullptr;
+        char* po = NORM && p.out ? p.out + row * p.ldo * ES : nullptr;
+        float h[VPT][8], hx = 0.0f;   // values past the end are 0: they change neither the sum nor the largest magnitude
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            const int c = (v * NT + t) * 8;
+            if (c < whole)
+                Elem<BF16>::load8(px + (size_t)c * ES, h[v]);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[v][e] = 0.0f;
+        }
+        if (t < over) hx = Elem<BF16>::load1(px + (size_t)(whole + t) * ES);
+        if (NORM && pr) {
+#pragma unroll
+            for (int v = 0; v < VPT; ++v) {
+                const int c = (v * NT + t) * 8;
+                if (c < whole) {
+                    float r[8];
+                    Elem<BF16>::load8(pr + (size_t)c * ES, r);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) h[v][e] += r[e];
+                }
+            }
+            if (t < over) hx += Elem<BF16>::load1(pr + (size_t)(whole + t) * ES);
+        }
+        if (NORM && po) {
+#pragma unroll
+            for (int v = 0; v < VPT; ++v) {
+                const int c = (v * NT + t) * 8;
+                if (c < whole) Elem<BF16>::store8(po + (size_t)c * ES, h[v]);
+            }
+            if (t < over) Elem<BF16>::store1(po + (size_t)(whole + t) * ES, hx);
+        }
+        bool bad = false;
+        if constexpr (NORM) {
+            float sum = hx * hx;
+#pragma unroll
+            for (int v = 0; v < VPT; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum = fmaf(h[v][e], h[v][e], sum);
+            sum = row_sum<NT>(sum, psum);
+            bad = (__float_as_uint(sum) & 0x7fffffffu) >= 0x7f800000u;
+            const float r = 1.0f / sqrtf(sum / (float)p.width + p.eps);
+#pragma unroll
+            for (int v = 0; v < VPT; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[v][e] *= r;
+            hx *= r;
+            if (p.gamma) {
+#pragma unroll
+                for (int v = 0; v < VPT; ++v) {
+                    const int c = (v * NT + t) * 8;
+                    if (c < whole) {
+                        float g[8];
+                        Elem<false>::load8((const char*)(p.gamma + c), g);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) h[v][e] *= g[e];
+                    }
+                }
+                if (t < over) hx *= p.gamma[whole + t];
+            }
+        }
+        // the largest magnitude as bits: a NaN is larger than infinity, which is larger than any number
+        unsigned most = __float_as_uint(hx) & 0x7fffffffu;
+#pragma unroll
+        for (int v = 0; v < VPT; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(h[v][e]) & 0x7fffffffu);
+        most = row_max<NT>(most, pmax);
+        bad = bad || most >= 0x7f800000u;
+        const float a = __uint_as_float(most);
+        const bool none = !(a >= 127.0f * 1.17549435e-38f);
+        const float inv = 127.0f / a;
+        if (t == 0) p.scales[row] = bad ? __uint_as_float(0x7fc00000u) : none ? 0.0f : a / 127.0f;
+        int8_t* pq = p.q + row * p.ldq;
+        const bool zero = bad || none;
+        // 1.5 * 2^23 + n holds n, rounded to nearest even by the addition, in its low bits
+        auto round8 = [&](float f) { return zero ? 0u : __float_as_uint(fmaf(f, inv, 12582912.0f)) & 0xffu; };
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            const int c = (v * NT + t) * 8;
+            if (c < whole) {
+                u32x2 w;
+                w[0] = round8(h[v][0]) | round8(h[v][1]) << 8 | round8(h[v][2]) << 16 | round8(h[v][3]) << 24;
+                w[1] = round8(h[v][4]) | round8(h[v][5]) << 8 | round8(h[v][6]) << 16 | round8(h[v][7]) << 24;
+                __builtin_memcpy(pq + c, &w, 8);
+            }
+        }
+        if (t < over) pq[whole + t] = (int8_t)round8(hx);
+    }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void q8_dequantize_kernel(const int8_t* q, int64_t ldq, const float* scales, char* y,
+                                                            int64_t ldy, int64_t rows, int width, int units)
+{
+    constexpr int ES = Elem<BF16>::kBytes;
+    const int64_t total = rows * units;   // of 8 values
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / units;
+        const int c = (int)(i - row * units) * 8;
+        const int8_t* pq = q + row * ldq + c;
+        char* py = y + (row * ldy + c) * ES;
+        const float s = scales[row];
+        if (c + 8 <= width) {
+            u32x2 w;
+            __builtin_memcpy(&w, pq, 8);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)(w[e / 4] >> (8 * (e % 4))) * s;
+            Elem<BF16>::store8(py, v);
+        } else {
+            for (int e = 0; c + e < width; ++e) Elem<BF16>::store1(py + (size_t)e * ES, (float)pq[e] * s);
+        }
+    }
+}
+
+template <bool BF16, int NT, int VPT>
+int launch_rows(const RowArgs& p, bool norm, hipStream_t s)
+{
+    constexpr int BLOCK = NT < 256 ? 256 : NT, RPB = BLOCK / NT;
+    const int64_t blocks = (p.rows + RPB - 1) / RPB;
+    const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
+    if (norm)
+        hipLaunchKernelGGL((q8_rows_kernel<BF16, NT, VPT, true>), dim3(grid), dim3(BLOCK), 0, s, p);
+    else
+        hipLaunchKernelGGL((q8_rows_kernel<BF16, NT, VPT, false>), dim3(grid), dim3(BLOCK), 0, s, p);
+    NM_HIP_CHECK(hipGetLastError());
+    return NM_OK;
+}
+
+template <bool BF16>
+int pick_rows(const RowArgs& p, bool norm, hipStream_t s)
+{
+    const int w = p.width;
+    if (w <= 512) return launch_rows<BF16, 64, 1>(p, norm, s);
+    if (w <= 1024) return launch_rows<BF16, 64, 2>(p, norm, s);
+    if (w <= 2048) return launch_rows<BF16, 256, 1>(p, norm, s);
+    if (w <= 4096) return launch_rows<BF16, 256, 2>(p, norm, s);
+    if (w <= 8192) return launch_rows<BF16, 256, 4>(p, norm, s);
+    if (w <= 16384) return launch_rows<BF16, 256, 8>(p, norm, s);
+    if (w <= 32768) return launch_rows<BF16, 1024, 4>(p, norm, s);
+    return launch_rows<BF16, 1024, 8>(p, norm, s);
+}
+
+}  // namespace
+
+int run_q8_rows(const void* x, nm_dtype_t dt, int64_t rows, int width, int64_t ldx, const void* res, int64_t ldr,
+                const float* gamma, float eps, bool norm, void* out, int64_t ldo, int8_t* q, int64_t ldq, float* scales,
+                hipStream_t s)
+{
+    RowArgs p{(const char*)x, (const char*)res, gamma, (char*)out, q, scales, rows, ldx, ldr, ldo, ldq, width, eps};
+    return dt == NM_F32 ? pick_rows<false>(p, norm, s) : pick_rows<true>(p, norm, s);
+}
+
+int run_q8_dequantize(const int8_t* q, int64_t ldq, const float* scales, int64_t rows, int width, void* y, nm_dtype_t dt,
+                      int64_t ldy, hipStream_t s)
+{
+    const int units = (width + 7) / 8;
+    const int64_t blocks = (rows * units + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
+    if (dt == NM_F32)
+        hipLaunchKernelGGL((q8_dequantize_kernel<false>), dim3(grid), dim3(256), 0, s, q, ldq, scales, (char*)y, ldy, rows, width, units);
+    else
+        hipLaunchKernelGGL((q8_dequantize_kernel<true>), dim3(grid), dim3(256), 0, s, q, ldq, scales, (char*)y, ldy, rows, width, units);
+    NM_HIP_CHECK(hipGetLastError());
+    return NM_OK;
+}
+
+}  // namespace nm
