@@ -24,6 +24,7 @@ _STATUS = {0: "NM_OK", -1: "NM_ERR_ARG", -2: "NM_ERR_SHAPE", -3: "NM_ERR_UNSUPPO
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libnmconv.so")
 _lib = None
+_torch = None   # the module, from the first lib() on
 
 
 class NMError(RuntimeError):
@@ -34,7 +35,7 @@ class NMError(RuntimeError):
 
 def lib():
     """Open libnmconv.so (once).  Raises if it has not been built."""
-    global _lib
+    global _lib, _torch
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(
@@ -43,7 +44,8 @@ def lib():
         # PyTorch ships its own copy of the HIP runtime; a process must not end up with two.
         # Importing torch first makes its copy the one libnmconv.so binds to as well (loaded
         # the other way round, torch finds no GPU).
-        import torch  # noqa: F401
+        import torch
+        _torch = torch
         L = ctypes.CDLL(LIB_PATH)
         ci, cf, vp = ctypes.c_int, ctypes.c_float, ctypes.c_void_p
         pi = ctypes.POINTER(ctypes.c_int)
@@ -413,6 +415,8 @@ def nm_variant_legal(v: int, wp: Packed, x_dtype: int = NM_F32, y_dtype: int = N
 
 
 # ---------------------------------------------------------------- 8-bit feed-forward operators (nm_q8.h)
+# A single token's call runs for a few us on the GPU, so these keep what they ask of a tensor short, and do not look at outputs
+# that they have allocated themselves.  A given stream is made the current one for the call: what is allocated then belongs to it.
 def _rows_of(t, name: str):
     """(rows, width, row stride) of a device tensor whose last axis is the row: two axes with any row stride, or any
     number of them contiguous."""
@@ -431,33 +435,52 @@ def _rows_of(t, name: str):
     return (t.numel() // width if width else 0), width, width
 
 
-def _q8_out(t, name: str, shape, dtype, like):
-    import torch
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+def _q8_stride(t, name: str, shape, dtype, like) -> int:
+    """Row stride of a tensor that the caller gave and that has to have this shape and type."""
     if t.shape != shape or t.dtype != dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {like.device}")
-    return t
+    return _rows_of(t, name)[2]
 
 
-def _q8_vector(t, name: str, n: int, like):
-    """Pointer of a contiguous fp32 vector of n values on the device of `like` (0 for None)."""
-    import torch
-    if t is None:
-        return 0
-    if t.dtype != torch.float32 or t.numel() != n or t.get_device() != like.get_device() or not t.is_contiguous():
+def _q8_vector(t, name: str, n: int, like) -> int:
+    """Pointer of a contiguous fp32 vector of n values on the device of `like`."""
+    if t.dtype != _torch.float32 or t.numel() != n or t.get_device() != like.get_device() or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous fp32 tensor of {n} values on {like.device}")
     return t.data_ptr()
 
 
+def _q8_scales(x, scales, rows: int):
+    """(scales of x's rows, pointer): the caller's or new ones."""
+    if scales is None:
+        scales = x.new_empty(x.shape[:-1], dtype=_torch.float32)
+        return scales, scales.data_ptr()
+    if scales.shape != x.shape[:-1]:
+        raise ValueError(f"scales must have the shape {tuple(x.shape[:-1])}")
+    return scales, _q8_vector(scales, "scales", rows, x)
+
+
+def _q8_like(x, dtype):
+    return _torch.empty_like(x, dtype=dtype, memory_format=_torch.contiguous_format)
+
+
+def _q8_stream() -> int:
+    return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice())
+
+
 def nm_quantize_q8(x, q=None, scales=None, stream=None):
     """Rows of x (fp32 or bf16, the last axis) rounded to 8 bits: (q int8 like x, scales fp32 [rows...]) with x ~ q * scales."""
-    import torch
+    L = _lib or lib()
+    if stream is not None:
+        with _torch.cuda.stream(stream):
+            return nm_quantize_q8(x, q, scales)
     rows, width, ld = _rows_of(x, "x")
-    q = _q8_out(q, "q", x.shape, torch.int8, x)
-    scales = _q8_out(scales, "scales", x.shape[:-1], torch.float32, x)
-    rc = (_lib or lib()).nm_quantize_q8(x.data_ptr(), _dtype_code(x), rows, width, ld, q.data_ptr(), _rows_of(q, "q")[2],
-                                        _q8_vector(scales, "scales", rows, x), _stream_ptr(stream))
+    ldq = width
+    if q is None:
+        q = _q8_like(x, _torch.int8)
+    else:
+        ldq = _q8_stride(q, "q", x.shape, _torch.int8, x)
+    scales, sptr = _q8_scales(x, scales, rows)
+    rc = L.nm_quantize_q8(x.data_ptr(), _dtype_code(x), rows, width, ld, q.data_ptr(), ldq, sptr, _q8_stream())
     if rc < 0:
         _check(rc)
     return q, scales
@@ -465,13 +488,20 @@ def nm_quantize_q8(x, q=None, scales=None, stream=None):
 
 def nm_dequantize_q8(q, scales, dtype=None, y=None, stream=None):
     """The values that 8-bit rows stand for, q * scales, in fp32 or bf16 (`dtype`; default fp32 or y's)."""
-    import torch
+    L = _lib or lib()
+    if stream is not None:
+        with _torch.cuda.stream(stream):
+            return nm_dequantize_q8(q, scales, dtype, y)
     rows, width, ld = _rows_of(q, "q")
-    if q.dtype != torch.int8:
+    if q.dtype != _torch.int8:
         raise TypeError(f"q must be int8, not {q.dtype}")
-    y = _q8_out(y, "y", q.shape, dtype or (torch.float32 if y is None else y.dtype), q)
-    rc = (_lib or lib()).nm_dequantize_q8(q.data_ptr(), ld, _q8_vector(scales, "scales", rows, q), rows, width, y.data_ptr(),
-                                          _dtype_code(y), _rows_of(y, "y")[2], _stream_ptr(stream))
+    ldy = width
+    if y is None:
+        y = _q8_like(q, dtype or _torch.float32)
+    else:
+        ldy = _q8_stride(y, "y", q.shape, dtype or y.dtype, q)
+    rc = L.nm_dequantize_q8(q.data_ptr(), ld, _q8_vector(scales, "scales", rows, q), rows, width, y.data_ptr(), _dtype_code(y), ldy,
+                            _q8_stream())
     if rc < 0:
         _check(rc)
     return y
@@ -480,23 +510,29 @@ def nm_dequantize_q8(q, scales, dtype=None, y=None, stream=None):
 def nm_rmsnorm_q8(x, gamma=None, residual=None, eps: float = 1e-6, q=None, scales=None, residual_out=None, stream=None):
     """h = x + residual; rows of gamma * h / sqrt(mean(h^2) + eps) rounded to 8 bits.  Returns (q, scales, h rounded to x's
     dtype); the last is None without a residual unless residual_out is given.  residual_out may be x or residual."""
-    import torch
+    L = _lib or lib()
+    if stream is not None:
+        with _torch.cuda.stream(stream):
+            return nm_rmsnorm_q8(x, gamma, residual, eps, q, scales, residual_out)
     rows, width, ld = _rows_of(x, "x")
-    ldr = rptr = ldo = optr = 0
+    dtype = x.dtype
+    ldr = rptr = optr = 0
+    ldq = ldo = width
     if residual is not None:
-        if residual.shape != x.shape or residual.dtype != x.dtype or residual.get_device() != x.get_device():
-            raise ValueError("residual must be shaped and typed like x")
-        ldr, rptr = _rows_of(residual, "residual")[2], residual.data_ptr()
-        if residual_out is None:
-            residual_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        ldr, rptr = _q8_stride(residual, "residual", x.shape, dtype, x), residual.data_ptr()
     if residual_out is not None:
-        residual_out = _q8_out(residual_out, "residual_out", x.shape, x.dtype, x)
-        ldo, optr = _rows_of(residual_out, "residual_out")[2], residual_out.data_ptr()
-    q = _q8_out(q, "q", x.shape, torch.int8, x)
-    scales = _q8_out(scales, "scales", x.shape[:-1], torch.float32, x)
-    rc = (_lib or lib()).nm_rmsnorm_q8(x.data_ptr(), _dtype_code(x), rows, width, ld, rptr, ldr, _q8_vector(gamma, "gamma", width, x),
-                                       eps, optr, ldo, q.data_ptr(), _rows_of(q, "q")[2], _q8_vector(scales, "scales", rows, x),
-                                       _stream_ptr(stream))
+        ldo, optr = _q8_stride(residual_out, "residual_out", x.shape, dtype, x), residual_out.data_ptr()
+    elif residual is not None:
+        residual_out = _q8_like(x, dtype)
+        optr = residual_out.data_ptr()
+    if q is None:
+        q = _q8_like(x, _torch.int8)
+    else:
+        ldq = _q8_stride(q, "q", x.shape, _torch.int8, x)
+    scales, sptr = _q8_scales(x, scales, rows)
+    rc = L.nm_rmsnorm_q8(x.data_ptr(), _dtype_code(x), rows, width, ld, rptr, ldr,
+                         0 if gamma is None else _q8_vector(gamma, "gamma", width, x), eps, optr, ldo, q.data_ptr(), ldq, sptr,
+                         _q8_stream())
     if rc < 0:
         _check(rc)
     return q, scales, residual_out
@@ -526,14 +562,17 @@ class Q8Weights:
 def nm_q8_pack(w, scales=None, gated: bool = False, stream=None) -> Q8Weights:
     """Weights [channels, width] on the device: int8 with fp32 scales [channels], or fp32 / bf16, which are rounded here
     (a scale for each channel).  gated: the first half of the channels gates the second."""
-    import torch
+    L = _lib or lib()
+    if stream is not None:
+        with _torch.cuda.stream(stream):
+            return nm_q8_pack(w, scales, gated)
     if w.dim() != 2:
         raise ValueError("w must have two axes")
     channels, width, ld = _rows_of(w, "w")
-    sptr = _q8_vector(scales, "scales", channels, w)
-    code = NM_I8 if w.dtype == torch.int8 else _dtype_code(w)
+    sptr = 0 if scales is None else _q8_vector(scales, "scales", channels, w)
+    code = NM_I8 if w.dtype == _torch.int8 else _dtype_code(w)
     h = ctypes.c_void_p()
-    _check(lib().nm_q8_pack(w.data_ptr(), code, sptr, channels, width, ld, int(bool(gated)), _stream_ptr(stream), ctypes.byref(h)))
+    _check(L.nm_q8_pack(w.data_ptr(), code, sptr, channels, width, ld, int(bool(gated)), _q8_stream(), ctypes.byref(h)))
     return Q8Weights(h, channels, width, bool(gated))
 
 
@@ -548,30 +587,34 @@ def nm_linear_q8(q, scales, w: Q8Weights, bias=None, residual=None, dtype=None, 
     """8-bit rows times 8-bit weights: (q @ w.T) * scales * channel scales + bias + residual, or the gated form
     silu(gate) * up.  y: [..., channels] (gated: half of them) in bf16 (default) or fp32; residual is typed and shaped
     like y and may be y."""
-    import torch
-    rows, width, ld = _rows_of(q, "q")
-    if q.dtype != torch.int8:
-        raise TypeError(f"q must be int8, not {q.dtype}")
     L = _lib or lib()
-    y = _q8_out(y, "y", q.shape[:-1] + (w.outs,), dtype or (torch.bfloat16 if y is None else y.dtype), q)
+    if stream is not None:
+        with _torch.cuda.stream(stream):
+            return nm_linear_q8(q, scales, w, bias, residual, dtype, y)
+    rows, width, ld = _rows_of(q, "q")
+    if q.dtype != _torch.int8:
+        raise TypeError(f"q must be int8, not {q.dtype}")
+    shape = q.shape[:-1] + (w.outs,)
+    ldy = w.outs
+    if y is None:
+        y = q.new_empty(shape, dtype=dtype or _torch.bfloat16)
+    else:
+        ldy = _q8_stride(y, "y", shape, dtype or y.dtype, q)
     ldr = rptr = 0
     if residual is not None:
-        if residual.shape != y.shape or residual.dtype != y.dtype or residual.get_device() != y.get_device():
-            raise ValueError("residual must be shaped and typed like the output")
-        ldr, rptr = _rows_of(residual, "residual")[2], residual.data_ptr()
+        ldr, rptr = _q8_stride(residual, "residual", shape, y.dtype, q), residual.data_ptr()
+    qptr = q.data_ptr()
     need = ctypes.c_size_t(0)
-    rc = L.nm_linear_q8_workspace(q.data_ptr(), rows, ld, w.handle, ctypes.byref(need))
+    rc = L.nm_linear_q8_workspace(qptr, rows, ld, w.handle, ctypes.byref(need))
     if rc < 0:
         _check(rc)
-    ws = wptr = None
-    if need.value:
-        ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+    wptr, nbytes = None, need.value
+    if nbytes:
+        ws = q.new_empty(nbytes)
         wptr = ws.data_ptr()
-        if stream is not None:
-            ws.record_stream(stream)
-    rc = L.nm_linear_q8(q.data_ptr(), rows, width, ld, _q8_vector(scales, "scales", rows, q), w.handle,
-                        _q8_vector(bias, "bias", w.channels, q), rptr, ldr, y.data_ptr(), _dtype_code(y), _rows_of(y, "y")[2],
-                        wptr, need.value, _stream_ptr(stream))
+    rc = L.nm_linear_q8(qptr, rows, width, ld, _q8_vector(scales, "scales", rows, q), w.handle,
+                        0 if bias is None else _q8_vector(bias, "bias", w.channels, q), rptr, ldr, y.data_ptr(), _dtype_code(y), ldy,
+                        wptr, nbytes, _q8_stream())
     if rc < 0:
         _check(rc)
     return y
