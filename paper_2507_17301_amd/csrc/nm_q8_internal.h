@@ -25,13 +25,14 @@ struct nm_q8 {
 namespace nm {
 
 // Channel (row of the caller's weight matrix) of packed row p, or -1 for padding.
-//   plain: block b, row 4 g + r of group G <-> channel 64 G + 16 g + 4 b + r      (16 adjacent channels a lane)
-//   gated: r < 2 the gate, r >= 2 the value of output 32 G + 8 g + 2 b + (r & 1)  (8 adjacent outputs a lane)
+//   plain: block b, row 4 g + r of group G <-> channel 64 G + 32 (b / 2) + 8 g + 4 (b & 1) + r  (twice 8 adjacent ones a lane)
+//   gated: r < 2 the gate, r >= 2 the value of output 32 G + 8 g + 2 b + (r & 1)                (8 adjacent outputs a lane)
+// Eight bf16 are the 16 bytes that a lane stores at once, and the four g of a row then store 64 adjacent bytes.
 __host__ __device__ inline int q8_row_of(int p, int channels, int gated)
 {
     const int G = p >> 6, b = (p >> 4) & 3, g = (p >> 2) & 3, r = p & 3;
     if (!gated) {
-        const int c = G * 64 + g * 16 + b * 4 + r;
+        const int c = G * 64 + (b >> 1) * 32 + g * 8 + (b & 1) * 4 + r;
         return c < channels ? c : -1;
     }
     const int o = G * 32 + g * 8 + b * 2 + (r & 1), half = channels / 2;
@@ -60,6 +61,7 @@ struct Q8Linear {
     int64_t ldq, ldr, ldy;
     int rows, width, channels, outs;   // outs: channels of y
     int gated, groups, kblocks, y_bf16;
+    int past;   // y is stored past the last-level cache
 };
 size_t q8_linear_workspace(const Q8Linear& p);
 int run_q8_linear(const Q8Linear& p, void* workspace, hipStream_t s);

@@ -6,176 +6,98 @@
 // 16x16x64 integer matrix instruction, rows of q the second: lane l of a wavefront then holds packed weight rows
 // 4 (l / 16) .. + 3 of a 16-row block for row l % 16 of q, and the packing deals channels so that the four blocks of
 // a 64-row group give it 16 adjacent channels (gated: 8 adjacent outputs, gate and value in the same registers).
-#include "nm_q8_device.h"
+#include "nm_q8_product.h"
 
 namespace nm {
 namespace {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
-
-__device__ inline __amdgpu_buffer_rsrc_t q8_rsrc(const void* p, unsigned bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
-}
-
-__device__ inline i32x4 mma(i32x4 w, i32x4 q, i32x4 acc) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(w, q, acc, 0, 0, 0); }
-
-// ---------------------------------------------------------------- epilogue
-// What a lane needs of the channels it holds over NB blocks (from block b0 on) of one row group.
-template <bool GATED, int NB> struct Channels {
-    static constexpr int kOuts = GATED ? 2 * NB : 4 * NB;   // adjacent outputs of a lane
-    int c0;                                                 // the first of them
-    f32x4 t[NB], bias[NB];
-
-    __device__ inline void load(const Q8Linear& p, int group, int b0, int lane)
-    {
-        const int g = lane >> 4, half = p.channels / 2;
-        c0 = GATED ? group * 32 + g * 8 + b0 * 2 : group * 64 + g * 16 + b0 * 4;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            t[b] = *reinterpret_cast<const f32x4*>(p.ws + group * 64 + (b0 + b) * 16 + g * 4);
-            bias[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (p.bias) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if constexpr (GATED) {
-                        const int o = c0 + 2 * b + (r & 1);
-                        if (o < half) bias[b][r] = p.bias[r < 2 ? o : half + o];
-                    } else {
-                        const int c = c0 + 4 * b + r;
-                        if (c < p.channels) bias[b][r] = p.bias[c];
-                    }
-                }
-            }
-        }
-    }
-};
-
-__device__ inline float silu_times(float gate, float up) { return gate / (1.0f + __expf(-gate)) * up; }
-
-// Scales the sums of one row of q and stores its outputs.
-template <bool GATED, bool BF16, int NB>
-__device__ inline void emit(const Q8Linear& p, const Channels<GATED, NB>& ch, const i32x4 (&acc)[NB], int64_t row, float s)
-{
-    constexpr int N = Channels<GATED, NB>::kOuts, ES = Elem<BF16>::kBytes;
-    float y[N];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        float z[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) z[r] = fmaf((float)acc[b][r], s * ch.t[b][r], ch.bias[b][r]);
-        if constexpr (GATED) {
-            y[2 * b] = silu_times(z[0], z[2]);
-            y[2 * b + 1] = silu_times(z[1], z[3]);
-        } else {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[4 * b + r] = z[r];
-        }
-    }
-    char* py = (char*)p.y + (row * p.ldy + ch.c0) * ES;
-    const char* pr = p.res ? (const char*)p.res + (row * p.ldr + ch.c0) * ES : nullptr;
-    if (N % 8 == 0 && ch.c0 + N <= p.outs) {
-#pragma unroll
-        for (int i = 0; i < N; i += 8) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = y[i + e];
-            if (!GATED && pr) {
-                float r[8];
-                Elem<BF16>::load8(pr + i * ES, r);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += r[e];
-            }
-            Elem<BF16>::store8(py + i * ES, v);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (ch.c0 + i < p.outs) {
-                float v = y[i];
-                if (!GATED && pr) v += Elem<BF16>::load1(pr + i * ES);
-                Elem<BF16>::store1(py + i * ES, v);
-            }
-        }
-    }
-}
-
 // ---------------------------------------------------------------- few rows
-// Up to 16 * TB rows of q.  A workgroup owns RB blocks of 16 packed channels; its NW wavefronts take the 64-k blocks in
-// turn, straight from memory into registers (a weight is used once, there is nothing to share), and add their sums
-// through LDS.  Bound by the weights' bytes.
-template <int TB, int RB, int NW, bool GATED, bool BF16>
+// Up to 16 * TB rows of q.  A workgroup owns RB blocks of 16 packed channels; its NW wavefronts take the steps of 128 k in turn,
+// U of them in flight each, and add their sums through LDS at the end.  Weights go from memory into registers: a weight is used
+// once, there is nothing to share.  Rows of q go through LDS, a part of it for each wavefront, so that 8 lanes read the 128
+// adjacent bytes of a row: read straight into operand registers, 16 rows with 64 bytes each an instruction, they come at a third
+// of the rate (38 instead of 120 bytes a ns and CU out of the L2), and 64 rows x 4096 x 4096 took 11.4 us instead of 8.7.
+// Bound by the weights' bytes: see pick_few for the times.
+template <int TB, int RB, int NW, int U> constexpr int few_lds()
+{
+    const int rows = NW * U * TB * 2048, sums = NW * RB * TB * 1024;
+    return rows > sums ? rows : sums;
+}
+
+template <int TB, int RB, int NW, int U, bool GATED, bool BF16>
 __global__ __launch_bounds__(NW * 64) void q8_few_kernel(Q8Linear p)
 {
-    constexpr int U = TB * RB >= 4 ? 2 : 4;   // k blocks in flight
-    __shared__ i32x4 part[NW][RB * TB][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t row0 = (int64_t)blockIdx.y * (16 * TB);
-    const int8_t* w[RB];
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int b0 = blockIdx.x * RB;   // (RB divides 4: a workgroup stays within its row group)
+    const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + (size_t)(b0 >> 2) * p.kblocks * 4096, (unsigned)p.kblocks * 4096);
+    const __amdgpu_buffer_rsrc_t qsr = q8_rsrc(p.q, rows_extent(p, p.rows));
+    const unsigned woff = (b0 & 3) * 1024 + lane * 16;
+    const unsigned mine = wave * (U * TB * 2048), lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem + mine;
+    const unsigned from = mine + (lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
+    unsigned qoff[TB][2];   // 8 rows an instruction, chunk c of a row at c ^ (row & 7)
+    bool there[TB][2];
 #pragma unroll
-    for (int i = 0; i < RB; ++i) {
-        const int rb = blockIdx.x * RB + i;   // (RB divides 4: a workgroup stays within its row group)
-        w[i] = p.w + ((size_t)(rb >> 2) * p.kblocks * 4 + (rb & 3)) * 1024 + lane * 16;
-    }
-    const int8_t* q[TB];
-    bool there[TB];
+    for (int i = 0; i < TB; ++i)
 #pragma unroll
-    for (int i = 0; i < TB; ++i) {
-        const int64_t row = row0 + i * 16 + (lane & 15);
-        there[i] = row < p.rows;
-        q[i] = p.q + (there[i] ? row : 0) * p.ldq + (lane >> 4) * 16;
-    }
-    const int kq = p.width - (lane >> 4) * 16;   // values of the row from this lane's first one on
+        for (int h = 0; h < 2; ++h) {
+            const int row = i * 16 + h * 8 + (lane >> 3);
+            there[i][h] = row < p.rows;
+            qoff[i][h] = (unsigned)(row * p.ldq) + (((lane & 7) ^ (lane >> 3)) << 4);
+        }
     i32x4 acc[RB][TB] = {};
-    for (int kb = wave; kb < p.kblocks; kb += NW * U) {
-        i32x4 wf[U][RB], qf[U][TB];
+    const int steps = p.kblocks / 2;
+    for (int k0 = wave; k0 < steps; k0 += NW * U) {
+        i32x4 wf[U][2][RB];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int k = kb + u * NW;
-            const bool in = k < p.kblocks;   // (the same for the whole wavefront)
+            const int k = k0 + u * NW;
+            const bool in = k < steps;   // past the last step nothing is read and zeros are multiplied
 #pragma unroll
-            for (int i = 0; i < RB; ++i) {
-                wf[u][i] = i32x4{0, 0, 0, 0};
-                if (in) wf[u][i] = *reinterpret_cast<const i32x4*>(w[i] + (size_t)k * 4096);
-            }
+            for (int i = 0; i < TB; ++i)
 #pragma unroll
-            for (int i = 0; i < TB; ++i) {
-                qf[u][i] = i32x4{0, 0, 0, 0};
-                if (there[i] && k * 64 + 16 <= kq) {
-                    __builtin_memcpy(&qf[u][i], q[i] + (size_t)k * 64, 16);
-                } else if (there[i] && k * 64 < kq) {
-                    for (int e = 0; e < kq - k * 64; ++e) {   // the row's end
-                        const int b = (int)(unsigned char)q[i][(size_t)k * 64 + e] << (8 * (e & 3));
+                for (int h = 0; h < 2; ++h)
+                    load_to_lds(qsr, in && there[i][h] ? qoff[i][h] + k * 128 : kPast, lds0 + u * TB * 2048 + i * 2048 + h * 1024);
 #pragma unroll
-                        for (int d = 0; d < 4; ++d) qf[u][i][d] |= (e >> 2) == d ? b : 0;
-                    }
-                }
-            }
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < RB; ++i)   // (nontemporal: no other workgroup reads them; 8 % faster)
+                    wf[u][h][i] = __builtin_bit_cast(
+                        i32x4, __builtin_amdgcn_raw_buffer_load_b128(wsr, in ? woff + i * 1024 + (k * 2 + h) * 4096 : kPast, 0, 2));
         }
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < RB; ++i)
+            for (int h = 0; h < 2; ++h) {
+                i32x4 qf[TB];
 #pragma unroll
-                for (int j = 0; j < TB; ++j) acc[i][j] = mma(wf[u][i], qf[u][j], acc[i][j]);
+                for (int j = 0; j < TB; ++j) qf[j] = *reinterpret_cast<const i32x4*>(smem + (from ^ (h * 64)) + u * TB * 2048 + j * 2048);
+#pragma unroll
+                for (int i = 0; i < RB; ++i)
+#pragma unroll
+                    for (int j = 0; j < TB; ++j) acc[i][j] = mma(wf[u][h][i], qf[j], acc[i][j]);
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // read, before the next loads land there
     }
+    __syncthreads();
+    i32x4* part = reinterpret_cast<i32x4*>(smem);   // [NW][RB * TB][64]
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int j = 0; j < TB; ++j) part[wave][i * TB + j][lane] = acc[i][j];
+        for (int j = 0; j < TB; ++j) part[(wave * RB * TB + i * TB + j) * 64 + lane] = acc[i][j];
     __syncthreads();
     for (int u = wave; u < RB * TB; u += NW) {
-        const int i = u / TB, j = u % TB, rb = blockIdx.x * RB + i;
-        i32x4 sum[1] = {part[0][u][lane]};
-#pragma unroll
-        for (int n = 1; n < NW; ++n) sum[0] += part[n][u][lane];
-        const int64_t row = row0 + j * 16 + (lane & 15);
+        const int i = u / TB, j = u % TB, rb = b0 + i;
+        const int row = j * 16 + (lane & 15);
         if (row < p.rows) {
             Channels<GATED, 1> ch;
             ch.load(p, rb >> 2, rb & 3, lane);
-            emit<GATED, BF16, 1>(p, ch, sum, row, p.qs[row]);
+            const float s = p.qs[row];
+            i32x4 sum[1] = {part[u * 64 + lane]};
+#pragma unroll
+            for (int n = 1; n < NW; ++n) sum[0] += part[(n * RB * TB + u) * 64 + lane];
+            emit<GATED, BF16, 1>(p, ch, sum, row, s);
         }
     }
 }
@@ -185,110 +107,144 @@ __global__ __launch_bounds__(NW * 64) void q8_few_kernel(Q8Linear p)
 // K goes by in steps of 128: both operands' next step is loaded straight into LDS while the present one is multiplied.
 // Weights lie in LDS as in memory (a wavefront's operand is 1 KiB of adjacent bytes); a row's 128 bytes are 8 chunks of 16,
 // chunk c stored at c ^ (row & 7), so that the 8 rows that an LDS cycle reads lie in 8 different places.
-// Needs q 16-byte aligned in address, stride and width.  What lies past a row's end meets zero weights; past the tensor's
-// end the buffer's bounds give zeros.
-template <int WR, int WT, int TB> struct Tile {
-    static constexpr int kWaves = WR * WT, kChannels = 64 * WR, kRows = 16 * TB * WT;
-    static constexpr int kWBytes = WR * 8192, kQBytes = kRows * 128, kStage = kWBytes + kQBytes, kLds = 2 * kStage;
-    static constexpr int kLoads = kStage / 1024 / kWaves;   // of 1 KiB, a wavefront and step
-    static_assert(kStage % (1024 * kWaves) == 0, "every wavefront issues the same number of loads");
+// SPLIT: blockIdx.y takes `per` of the K steps and stores its integer sums as they lie in the registers,
+//   part[split][tile][wave][16-row block][4 blocks][64 lanes], for q8_join_kernel to add and scale.
+template <int WR, int WT, int TB, int NS> struct Tile {
+    static constexpr int kWaves = WR * WT, kRows = 16 * TB * WT;
+    static constexpr int kWBytes = WR * 8192, kQBytes = kRows * 128, kStage = kWBytes + kQBytes, kLds = NS * kStage;
+    static constexpr int kLoads = kStage / 1024 / kWaves, kWLoads = kWBytes / 1024 / kWaves;   // of 1 KiB, a wavefront and step
+    static_assert(kWBytes % (1024 * kWaves) == 0 && kQBytes % (1024 * kWaves) == 0, "every wavefront issues the same loads");
 };
 
-// 16 bytes a lane from memory to LDS at `lds` + 16 * lane.  In asm, so that the compiler does not put a wait for it in front of
-// every read of LDS; the kernel waits for it itself.  (m0 is not one of the registers that the compiler hands out.)
-__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t r, unsigned voff, unsigned lds)
+template <int WR, int WT, int TB, int NS, bool SPLIT, bool GATED, bool BF16>
+__global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileOrder order, int per, i32x4* part)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(voff), "s"(r) : "memory");
-}
-
-template <int WR, int WT, int TB, bool GATED, bool BF16>
-__global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, int tiles_c, int tiles_r)
-{
-    using T = Tile<WR, WT, TB>;
+    using T = Tile<WR, WT, TB, NS>;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wr = wave % WR, wt = wave / WR;
-    const int tc = blockIdx.x % tiles_c, tr = blockIdx.x / tiles_c;
+    int tc, tr, tile;
+    if (!order.at(blockIdx.x, tc, tr, tile)) return;
     const int g0 = tc * WR;
     const int64_t row0 = (int64_t)tr * T::kRows;
     const int nrow = (int)(p.rows - row0 < T::kRows ? p.rows - row0 : T::kRows);
     const int ngrp = p.groups - g0 < WR ? p.groups - g0 : WR;
+    const int first = SPLIT ? blockIdx.y * per : 0;
+    const int steps = SPLIT ? (p.kblocks / 2 - first < per ? p.kblocks / 2 - first : per) : p.kblocks / 2;
     const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + (size_t)g0 * p.kblocks * 4096, (unsigned)ngrp * p.kblocks * 4096);
-    const __amdgpu_buffer_rsrc_t qsr = q8_rsrc(p.q + row0 * p.ldq, (unsigned)((nrow - 1) * p.ldq + p.width));
+    const __amdgpu_buffer_rsrc_t qsr = q8_rsrc(p.q + row0 * p.ldq, rows_extent(p, nrow));
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem;
     unsigned voff[T::kLoads];
 #pragma unroll
     for (int i = 0; i < T::kLoads; ++i) {
         const int c = wave + i * T::kWaves;   // 1 KiB of the stage
-        if (c < T::kWBytes / 1024) {
-            voff[i] = (unsigned)(c >> 3) * p.kblocks * 4096 + (c & 7) * 1024 + lane * 16;
+        if (i < T::kWLoads) {
+            voff[i] = ((unsigned)(c >> 3) * p.kblocks + first * 2) * 4096 + (c & 7) * 1024 + lane * 16;
         } else {
             const int row = (c - T::kWBytes / 1024) * 8 + (lane >> 3);
-            voff[i] = (unsigned)(row * p.ldq) + (((lane & 7) ^ (row & 7)) << 4);
+            voff[i] = (unsigned)(row * p.ldq) + first * 128 + (((lane & 7) ^ (row & 7)) << 4);
         }
     }
-    auto fetch = [&](int stage) {
-#pragma unroll
-        for (int i = 0; i < T::kLoads; ++i) {
-            const int c = wave + i * T::kWaves;
-            const bool weights = c < T::kWBytes / 1024;
-            load_to_lds(weights ? wsr : qsr, voff[i], lds0 + stage * T::kStage + c * 1024);
-            voff[i] += weights ? 8192 : 128;
-        }
+    auto fetch = [&](int i, unsigned at, bool there) {   // load i of a stage; past the last step nothing is read, so that the count of loads holds
+        const int c = wave + i * T::kWaves;
+        const bool weights = i < T::kWLoads;
+        load_to_lds(weights ? wsr : qsr, there ? voff[i] : kPast, lds0 + at + c * 1024);
+        voff[i] += weights ? 8192 : 128;
     };
-    i32x4 acc[TB][4] = {};
-    const int steps = p.kblocks / 2;
-    fetch(0);
     const int wlane = wr * 8192 + lane * 16;
     const int qlane = T::kWBytes + (wt * TB * 16 + (lane & 15)) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
+    i32x4 f[2][4 + TB];   // operands of the two halves of a step: 4 blocks of weights, TB of rows
+    auto read = [&](int h, int i, unsigned at) {
+        f[h][i] = *reinterpret_cast<const i32x4*>(smem + at + (i < 4 ? wlane + h * 4096 + i * 1024 : (qlane ^ (h * 64)) + (i - 4) * 2048));
+    };
+    i32x4 acc[TB][4] = {};
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int i = 0; i < T::kLoads; ++i) fetch(i, s * T::kStage, s < steps);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((NS - 1) * T::kLoads) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4 + TB; ++i) read(0, i, 0);
+    unsigned now = 0;   // the stage that is multiplied
     for (int k = 0; k < steps; ++k) {
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
-        if (k + 1 < steps) fetch((k + 1) & 1);
-        const char* st = smem + (k & 1) * T::kStage;
+        const unsigned next = now + T::kStage == T::kLds ? 0 : now + T::kStage;
+        // first half: its operands are in registers; the second half's are read meanwhile
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x4 wf[4], qf[TB];
+        for (int j = 0; j < TB; ++j) {
 #pragma unroll
-            for (int b = 0; b < 4; ++b) wf[b] = *reinterpret_cast<const i32x4*>(st + wlane + h * 4096 + b * 1024);
+            for (int i = j * (4 + TB) / TB; i < (j + 1) * (4 + TB) / TB; ++i) read(1, i, now);
 #pragma unroll
-            for (int j = 0; j < TB; ++j) qf[j] = *reinterpret_cast<const i32x4*>(st + (qlane ^ (h * 64)) + j * 2048);
-#pragma unroll
-            for (int j = 0; j < TB; ++j)
-#pragma unroll
-                for (int b = 0; b < 4; ++b) acc[j][b] = mma(wf[b], qf[j], acc[j][b]);
+            for (int b = 0; b < 4; ++b) acc[j][b] = mma(f[0][b], f[0][4 + j], acc[j][b]);
+            __builtin_amdgcn_sched_barrier(0);
         }
-    }
-    if (g0 + wr >= p.groups) return;
-    Channels<GATED, 4> ch;
-    ch.load(p, g0 + wr, 0, lane);
+        // this stage has been read, the next one has landed
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((NS - 2) * T::kLoads) : "memory");
+        // second half: the next step's first operands are read, the stage after the last one in LDS is loaded in this one's place
 #pragma unroll
-    for (int j = 0; j < TB; ++j) {
-        const int64_t row = row0 + (wt * TB + j) * 16 + (lane & 15);
-        if (row < p.rows) emit<GATED, BF16, 4>(p, ch, acc[j], row, p.qs[row]);
+        for (int j = 0; j < TB; ++j) {
+#pragma unroll
+            for (int i = j * (4 + TB) / TB; i < (j + 1) * (4 + TB) / TB; ++i) read(0, i, next);
+#pragma unroll
+            for (int i = j * T::kLoads / TB; i < (j + 1) * T::kLoads / TB; ++i) fetch(i, now, k + NS < steps);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) acc[j][b] = mma(f[1][b], f[1][4 + j], acc[j][b]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        now = next;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // no load into LDS outlives the workgroup
+    if constexpr (SPLIT) {
+        if (g0 + wr >= p.groups) return;
+        i32x4* to = part + ((size_t)(blockIdx.y * order.tiles_c * order.tiles_r + tile) * T::kWaves + wave) * TB * 256 + lane;
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
+            if (wt * TB * 16 + j * 16 < nrow)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) to[(j * 4 + b) * 64] = acc[j][b];
+    } else {
+        const int group = g0 + wr < p.groups ? g0 + wr : p.groups - 1;   // (what a wavefront past the last group has is not stored)
+        Channels<GATED, 4> ch;
+        ch.load(p, group, 0, lane);
+        constexpr int kFit = T::kLds / (16 * WT * 64 * WR * 4 / (GATED ? 2 : 1));   // blocks of rows that fit LDS in fp32
+        constexpr int JP4 = kFit >= TB ? TB : kFit >= TB / 2 ? TB / 2 : TB / 4, JP2 = 2 * kFit >= TB ? TB : TB / 2;
+        static_assert(JP4 <= kFit && JP2 <= 2 * kFit, "the tile's outputs go through LDS");
+        if (!BF16 || p.res) store_tile<WR, WT, TB, JP4, true, GATED, BF16>(p, ch, acc, smem, wr, wt, lane, g0, row0);
+        else store_tile<WR, WT, TB, JP2, false, GATED, BF16>(p, ch, acc, smem, wr, wt, lane, g0, row0);
     }
 }
 
-// Rows copied to 16-byte aligned ones of `pitch` bytes (the bytes past a row's end are zero).
-__global__ __launch_bounds__(256) void q8_align_kernel(const int8_t* q, int64_t ldq, int8_t* to, int pitch, int64_t rows, int width)
+// Adds the sums of `splits` parts and stores the results: a wavefront takes 16 rows x 64 packed channels.
+template <int WR, int WT, int TB, int NS, bool GATED, bool BF16>
+__global__ __launch_bounds__(256) void q8_join_kernel(Q8Linear p, TileOrder order, int splits, const i32x4* part)
 {
-    const int units = pitch / 16;
-    const int64_t total = rows * units;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / units;
-        const int c = (int)(i - row * units) * 16;
-        const int8_t* src = q + row * ldq + c;
-        i32x4 v = {0, 0, 0, 0};
-        if (c + 16 <= width) {
-            __builtin_memcpy(&v, src, 16);
-        } else {
-            for (int e = 0; c + e < width; ++e) {
-                const int b = (int)(unsigned char)src[e] << (8 * (e & 3));
+    using T = Tile<WR, WT, TB, NS>;
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int block = (int)(unit / (T::kWaves * TB)), wave = (int)(unit / TB) % T::kWaves, j = (int)(unit % TB);
+    int tc, tr, tile;
+    if (!order.at(block, tc, tr, tile)) return;
+    const int group = tc * WR + wave % WR;
+    const int64_t row = (int64_t)tr * T::kRows + ((wave / WR) * TB + j) * 16 + (lane & 15);
+    if (group >= p.groups || row >= p.rows) return;
+    const i32x4* from = part + (((size_t)tile * T::kWaves + wave) * TB + j) * 256 + lane;
+    const size_t next = (size_t)order.tiles_c * order.tiles_r * T::kWaves * TB * 256;
+    Channels<GATED, 4> ch;
+    ch.load(p, group, 0, lane);
+    const float s = p.qs[row];
+    i32x4 acc[4] = {};
+    for (int i = 0; i < splits; ++i, from += next)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) v[d] |= (e >> 2) == d ? b : 0;
-            }
-        }
-        *reinterpret_cast<i32x4*>(to + row * pitch + c) = v;
-    }
+        for (int b = 0; b < 4; ++b) acc[b] += from[b * 64];
+    emit<GATED, BF16, 4>(p, ch, acc, row, s);
+}
+
+// Rows copied to ones at a stride of `pitch` bytes, a multiple of 16 (the bytes past a row's end are zero).
+__global__ __launch_bounds__(256) void q8_align_kernel(const int8_t* q, int64_t ldq, int8_t* to, int pitch, int rows, int width)
+{
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 16;
+    if (c >= pitch) return;
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y)
+        *reinterpret_cast<i32x4*>(to + row * pitch + c) = load16(q + row * ldq + c, width - c);
 }
 
 // ---------------------------------------------------------------- weights
@@ -303,20 +259,7 @@ __global__ __launch_bounds__(256) void q8_pack_kernel(const int8_t* w, int64_t l
         const int kb = (int)(gk % kblocks), group = (int)(gk / kblocks);
         const int c = q8_row_of(group * 64 + b * 16 + (lane & 15), channels, gated);
         const int k = kb * 64 + (lane >> 4) * 16;
-        i32x4 v = {0, 0, 0, 0};
-        if (c >= 0 && k < width) {
-            const int8_t* src = w + c * ldw + k;
-            if (k + 16 <= width) {
-                __builtin_memcpy(&v, src, 16);
-            } else {
-                for (int e = 0; k + e < width; ++e) {
-                    const int byte = (int)(unsigned char)src[e] << (8 * (e & 3));
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) v[d] |= (e >> 2) == d ? byte : 0;
-                }
-            }
-        }
-        *reinterpret_cast<i32x4*>(to + i * 16) = v;
+        *reinterpret_cast<i32x4*>(to + i * 16) = load16(w + (int64_t)c * ldw + k, c < 0 ? 0 : width - k);
         if (kb == 0 && (lane >> 4) == 0) {
             const float s = c >= 0 ? scales[c] : 0.0f;
             if (!(fabsf(s) < INFINITY)) atomicOr(bad, 1);
@@ -346,66 +289,180 @@ __global__ void q8_clear_kernel(int* p) { *p = 0; }
 // ---------------------------------------------------------------- launches
 constexpr int kFewRows = 64;
 
-inline bool aligned16(const Q8Linear& p) { return (uintptr_t)p.q % 16 == 0 && p.ldq % 16 == 0 && p.width % 16 == 0; }
-inline int padded(int width) { return (width + 127) / 128 * 128; }
+// Whether the kernels can read q where it lies.
+inline bool aligned16(const Q8Linear& p) { return (uintptr_t)p.q % 16 == 0 && (p.rows == 1 || p.ldq % 16 == 0); }
 
-template <int TB, int RB, int NW, bool GATED, bool BF16>
+template <int TB, int RB, int NW, int U, bool GATED, bool BF16>
 int launch_few(const Q8Linear& p, hipStream_t s)
 {
-    const dim3 grid((unsigned)(p.groups * 4 / RB), (unsigned)((p.rows + 16 * TB - 1) / (16 * TB)));
-    hipLaunchKernelGGL((q8_few_kernel<TB, RB, NW, GATED, BF16>), grid, dim3(NW * 64), 0, s, p);
+    constexpr int LDS = few_lds<TB, RB, NW, U>();
+    static_assert(LDS <= 64 * 1024, "more needs allow_lds");
+    hipLaunchKernelGGL((q8_few_kernel<TB, RB, NW, U, GATED, BF16>), dim3((unsigned)(p.groups * 4 / RB)), dim3(NW * 64), LDS, s, p);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }
 
-template <int WR, int WT, int TB, bool GATED, bool BF16>
-int launch_tile(const Q8Linear& p, hipStream_t s)
+// More channels a workgroup read q less often, fewer make more workgroups; 256 CUs want two or more each.  us at width 4096, one row,
+// 16, 32, 64 rows, with 1 / 2 / 4 blocks of channels a workgroup:
+//    4096 channels   5.7 / 5.8 /  7.8    5.7 / 6.5 /  8.5     6.5 /  7.8 / 10.1     8.7 / 10.0 / 12.9
+//    8192            8.8 / 8.8 /  8.4    8.9 / 8.8 /  8.9    10.4 /  9.3 / 10.4    14.7 / 10.8 / 13.3
+//   12288           11.4 / 11.2 / 10.0  12.0 / 12.0 / 10.2   14.8 / 13.7 / 11.5    20.4 / 17.7 / 14.3
+//   24576           20.0 / 19.4 / 17.9  22.1 / 19.6 / 18.6   27.8 / 21.3 / 20.1    38.5 / 26.5 / 24.2
+// (16.8, 33.6, 50.3 and 100.7 MB of weights, out of HBM.)
+template <int TB, bool GATED, bool BF16>
+int pick_few(const Q8Linear& p, hipStream_t s)
 {
-    using T = Tile<WR, WT, TB>;
+    constexpr int U = TB == 4 ? 1 : 2;
+    if (p.groups >= 192) return launch_few<TB, 4, 4, U, GATED, BF16>(p, s);
+    if (p.groups >= 128) return launch_few<TB, 2, 8, U, GATED, BF16>(p, s);
+    return launch_few<TB, 1, 8, U, GATED, BF16>(p, s);
+}
+
+// The tile kernels' shapes.
+struct Shape {
+    int waves, wr, rows, tb;
+    int per_cu;                  // workgroups that a CU holds (by LDS)
+    float fixed, step1, step;    // us: of a round; of a K step with one workgroup a CU, with per_cu of them
+};
+constexpr Shape kShapes[] = {{8, 4, 256, 8, 1, 10.0f, 1.45f, 1.45f},    // 256 channels x 256 rows
+                             {4, 2, 128, 4, 2, 6.0f, 0.83f, 1.09f},     // 128 x 128, two stages
+                             {4, 2, 128, 4, 1, 6.5f, 0.54f, 0.54f},     // 128 x 128, three stages
+                             {2, 2, 64, 4, 2, 6.2f, 0.42f, 0.70f}};     // 128 x 64
+
+// What runs a call: a tile shape and the parts that K is cut into.
+struct Plan {
+    int shape = -1;    // -1: the few-row kernels
+    int splits = 1;
+    int per = 0;       // K steps of a part
+};
+
+inline TileOrder order_of(const Q8Linear& p, int shape)
+{
+    TileOrder o;
+    o.tiles_c = (p.groups + kShapes[shape].wr - 1) / kShapes[shape].wr;
+    o.tiles_r = (int)(((int64_t)p.rows + kShapes[shape].rows - 1) / kShapes[shape].rows);
+    o.per_xcd = (o.tiles_c * o.tiles_r + 7) / 8;
+    return o;
+}
+
+// The shape and split with the least estimated time: rounds of workgroups over the 256 CUs, each a fixed part and its K steps; for a
+// split the second kernel and its traffic.  The figures of kShapes are fitted to timings of 64 to 4096 rows on 1000 to 32768 channels of
+// 1040 to 12288 values, and the estimate is within 15 % of them.
+Plan plan_linear(const Q8Linear& p)
+{
+    Plan best;
+    if (p.rows <= kFewRows) return best;
+    const int steps = p.kblocks / 2;
+    float least = 1e30f;
+    for (int sh = 0; sh < 4; ++sh) {
+        const Shape& k = kShapes[sh];
+        const TileOrder o = order_of(p, sh);
+        const int64_t tiles = (int64_t)o.tiles_c * o.tiles_r;
+        for (int splits = 1; splits <= 16 && splits <= steps; ++splits) {
+            if (splits > 1 && tiles * splits > 512) break;
+            const int per = (steps + splits - 1) / splits;
+            if ((splits - 1) * per >= steps) continue;   // (an empty part)
+            const int64_t wgs = tiles * splits;
+            const float rounds = (float)((wgs + 256 * k.per_cu - 1) / (256 * k.per_cu));
+            float us = rounds * (k.fixed + per * (wgs <= 256 ? k.step1 : k.step));
+            if (splits > 1) us += 1.5f + 0.33e-6f * 4.0f * splits * p.rows * p.groups * 64;
+            if (us < least) {
+                least = us;
+                best.shape = sh;
+                best.splits = splits;
+                best.per = per;
+            }
+        }
+    }
+    return best;
+}
+
+inline size_t part_bytes(const Q8Linear& p, const Plan& pl)
+{
+    const TileOrder o = order_of(p, pl.shape);
+    return (size_t)pl.splits * o.tiles_c * o.tiles_r * kShapes[pl.shape].waves * kShapes[pl.shape].tb * 4096;
+}
+
+template <int SHAPE, int WT, int NS, bool GATED, bool BF16>
+int launch_tile(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
+{
+    constexpr int WR = kShapes[SHAPE].wr, TB = kShapes[SHAPE].tb;
+    using T = Tile<WR, WT, TB, NS>;
+    static_assert(T::kWaves == kShapes[SHAPE].waves && T::kRows == kShapes[SHAPE].rows, "kShapes describes the kernels");
+    const TileOrder o = order_of(p, SHAPE);
+    const dim3 grid((unsigned)o.per_xcd * 8, (unsigned)pl.splits);
+    if (pl.splits == 1) {
+        static unsigned long long done = 0;
+        const int rc = allow_lds((const void*)q8_tile_kernel<WR, WT, TB, NS, false, GATED, BF16>, T::kLds, &done);
+        if (rc != NM_OK) return rc;
+        hipLaunchKernelGGL((q8_tile_kernel<WR, WT, TB, NS, false, GATED, BF16>), grid, dim3(T::kWaves * 64), T::kLds, s, p, o, 0, (i32x4*)nullptr);
+        NM_HIP_CHECK(hipGetLastError());
+        return NM_OK;
+    }
     static unsigned long long done = 0;
-    const int rc = allow_lds((const void*)q8_tile_kernel<WR, WT, TB, GATED, BF16>, T::kLds, &done);
+    const int rc = allow_lds((const void*)q8_tile_kernel<WR, WT, TB, NS, true, false, false>, T::kLds, &done);
     if (rc != NM_OK) return rc;
-    const int tiles_c = (p.groups + WR - 1) / WR, tiles_r = (int)(((int64_t)p.rows + T::kRows - 1) / T::kRows);
-    hipLaunchKernelGGL((q8_tile_kernel<WR, WT, TB, GATED, BF16>), dim3((unsigned)tiles_c * tiles_r), dim3(T::kWaves * 64), T::kLds, s, p,
-                       tiles_c, tiles_r);
+    hipLaunchKernelGGL((q8_tile_kernel<WR, WT, TB, NS, true, false, false>), grid, dim3(T::kWaves * 64), T::kLds, s, p, o, pl.per, (i32x4*)part);
+    NM_HIP_CHECK(hipGetLastError());
+    hipLaunchKernelGGL((q8_join_kernel<WR, WT, TB, NS, GATED, BF16>), dim3((unsigned)o.per_xcd * 8 * T::kWaves * TB / 4), dim3(256), 0, s, p, o,
+                       pl.splits, (const i32x4*)part);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }
 
 template <bool GATED, bool BF16>
-int pick_linear(const Q8Linear& p, hipStream_t s)
+int pick_linear(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
 {
-    if (p.rows <= 16) return launch_few<1, 1, 8, GATED, BF16>(p, s);
-    if (p.rows <= 32) return launch_few<2, 1, 8, GATED, BF16>(p, s);
-    if (p.rows <= kFewRows) return launch_few<4, 1, 8, GATED, BF16>(p, s);
-    const int64_t big = (int64_t)((p.groups + 3) / 4) * ((p.rows + 255) / 256);
-    if (big >= 192) return launch_tile<4, 2, 8, GATED, BF16>(p, s);
-    return launch_tile<2, 2, 4, GATED, BF16>(p, s);
+    switch (pl.shape) {
+    case 0: return launch_tile<0, 2, 2, GATED, BF16>(p, pl, part, s);
+    case 1: return launch_tile<1, 2, 2, GATED, BF16>(p, pl, part, s);
+    case 2: return launch_tile<2, 2, 3, GATED, BF16>(p, pl, part, s);
+    case 3: return launch_tile<3, 1, 3, GATED, BF16>(p, pl, part, s);
+    default: break;
+    }
+    if (p.rows <= 16) return pick_few<1, GATED, BF16>(p, s);
+    if (p.rows <= 32) return pick_few<2, GATED, BF16>(p, s);
+    return pick_few<4, GATED, BF16>(p, s);
+}
+
+// The workspace: rows of q at a stride that the kernels can read, if theirs is none, then the parts of a split sum.
+struct Layout {
+    Plan plan;
+    size_t rows_bytes = 0, part_bytes = 0;
+    int pitch = 0;
+};
+Layout layout_of(const Q8Linear& p)
+{
+    Layout l;
+    l.plan = plan_linear(p);
+    l.pitch = (p.width + 15) / 16 * 16;
+    if (!aligned16(p)) l.rows_bytes = (size_t)p.rows * l.pitch;
+    if (l.plan.splits > 1) l.part_bytes = part_bytes(p, l.plan);
+    return l;
 }
 
 }  // namespace
 
 size_t q8_linear_workspace(const Q8Linear& p)
 {
-    if (p.rows <= kFewRows || aligned16(p)) return 0;
-    return (size_t)p.rows * padded(p.width);
+    const Layout l = layout_of(p);
+    return l.rows_bytes + l.part_bytes;
 }
 
 int run_q8_linear(const Q8Linear& call, void* workspace, hipStream_t s)
 {
     Q8Linear p = call;
-    if (q8_linear_workspace(p)) {
-        const int pitch = padded(p.width);
-        const int64_t blocks = ((int64_t)p.rows * (pitch / 16) + 255) / 256;
-        hipLaunchKernelGGL(q8_align_kernel, dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20))), dim3(256), 0, s, p.q, p.ldq,
-                           (int8_t*)workspace, pitch, (int64_t)p.rows, p.width);
+    const Layout l = layout_of(p);
+    if (l.rows_bytes) {
+        const dim3 grid((unsigned)(l.pitch / 16 + 255) / 256, (unsigned)(p.rows < 4096 ? p.rows : 4096));
+        hipLaunchKernelGGL(q8_align_kernel, grid, dim3(256), 0, s, p.q, p.ldq, (int8_t*)workspace, l.pitch, p.rows, p.width);
         NM_HIP_CHECK(hipGetLastError());
         p.q = (const int8_t*)workspace;
-        p.ldq = pitch;
-        p.width = pitch;
+        p.ldq = l.pitch;
     }
-    if (p.gated) return p.y_bf16 ? pick_linear<true, true>(p, s) : pick_linear<true, false>(p, s);
-    return p.y_bf16 ? pick_linear<false, true>(p, s) : pick_linear<false, false>(p, s);
+    void* part = (char*)workspace + l.rows_bytes;
+    if (p.gated) return p.y_bf16 ? pick_linear<true, true>(p, l.plan, part, s) : pick_linear<true, false>(p, l.plan, part, s);
+    return p.y_bf16 ? pick_linear<false, true>(p, l.plan, part, s) : pick_linear<false, false>(p, l.plan, part, s);
 }
 
 int run_q8_pack(const int8_t* w, int64_t ldw, const float* scales, const nm_q8* h, int* d_bad, hipStream_t s)
