@@ -12,7 +12,7 @@
  * calling thread's current device, allocate nothing and never wait, and may be captured
  * into a graph -- except nm_q8_pack and the exports, which are synchronous.
  *
- * Rows, widths and strides: 0 <= rows <= 2^31 - 1 (a call with no rows checks its
+ * Rows, widths and strides: 0 <= rows <= 2^30 (a call with no rows checks its
  * arguments and enqueues nothing), 1 <= width <= NM_Q8_MAX_WIDTH.  An input's rows may
  * overlap or be one and the same (stride 0); an output's must not.  Strides are at most
  * 2^24 elements.  fp32 and bf16 pointers need the alignment of their element only.
@@ -107,7 +107,8 @@ int nm_q8_export(const nm_q8_t* w, int8_t* w_host, float* scales_host);
  *   y_rc = z_rc / (1 + exp(-z_rc)) * z_r,(c+C)   gated weights of 2 C channels (no residual)
  * rounded to nearest even once if y_dtype is NM_BF16.  The result does not depend on the
  * other rows of the call nor on how the sum was divided.
- *   q_dev, ldq      int8 rows of the weights' width at any stride >= 0, any alignment
+ *   q_dev, ldq      int8 rows of the weights' width at any stride >= 0, any alignment.  The aligned 16 bytes that hold a
+ *                   row's last value are read as a whole.
  *   scales_dev      fp32 [rows]
  *   bias_dev        fp32 [channels] (gated: gates first, as the weights), or NULL
  *   residual_dev    rows of y_dtype at stride ldr, or NULL.  It may be y_dev itself (same stride).
@@ -120,7 +121,9 @@ int nm_linear_q8(const int8_t* q_dev, int64_t rows, int width, int64_t ldq, cons
                  const float* bias_dev, const void* residual_dev, int64_t ldr, void* y_dev, nm_dtype_t y_dtype,
                  int64_t ldy, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
-/* Bytes of workspace that nm_linear_q8 needs for these arguments; 0 for most. */
+/* Bytes of workspace that nm_linear_q8 needs for these arguments: for rows that do not start at multiples of 16 bytes (address and, with
+ * more than one row, stride), and for sums divided over workgroups.  0 for up to NM_Q8_FEW_ROWS rows that do start there. */
+enum { NM_Q8_FEW_ROWS = 64 };
 int nm_linear_q8_workspace(const int8_t* q_dev, int64_t rows, int64_t ldq, const nm_q8_t* w, size_t* bytes);
 
 #ifdef __cplusplus

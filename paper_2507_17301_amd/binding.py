@@ -15,7 +15,7 @@ from typing import Optional, Tuple
 import numpy as np
 
 NM_F32, NM_BF16, NM_F8E4M3, NM_I8 = 0, 1, 2, 3
-NM_Q8_MAX_WIDTH = 65536
+NM_Q8_MAX_WIDTH, NM_Q8_FEW_ROWS = 65536, 64
 NM_OK = 0
 NM_ERR_ARG, NM_ERR_SHAPE, NM_ERR_UNSUPPORTED, NM_ERR_ALLOC, NM_ERR_HIP, NM_ERR_IO = -1, -2, -3, -4, -5, -6
 _STATUS = {0: "NM_OK", -1: "NM_ERR_ARG", -2: "NM_ERR_SHAPE", -3: "NM_ERR_UNSUPPORTED",
@@ -25,6 +25,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libnmconv.so")
 _lib = None
 _torch = None   # the module, from the first lib() on
+_q8_codes = {}  # element types that the 8-bit operators know, from then on
 
 
 class NMError(RuntimeError):
@@ -46,6 +47,7 @@ def lib():
         # the other way round, torch finds no GPU).
         import torch
         _torch = torch
+        _q8_codes.update({torch.float32: NM_F32, torch.bfloat16: NM_BF16, torch.int8: NM_I8})
         L = ctypes.CDLL(LIB_PATH)
         ci, cf, vp = ctypes.c_int, ctypes.c_float, ctypes.c_void_p
         pi = ctypes.POINTER(ctypes.c_int)
@@ -419,7 +421,7 @@ def nm_variant_legal(v: int, wp: Packed, x_dtype: int = NM_F32, y_dtype: int = N
 # that they have allocated themselves.  A given stream is made the current one for the call: what is allocated then belongs to it.
 def _rows_of(t, name: str):
     """(rows, width, row stride) of a device tensor whose last axis is the row: two axes with any row stride, or any
-    number of them contiguous."""
+    number of them whose rows lie at one stride."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     shape = t.shape
@@ -429,10 +431,22 @@ def _rows_of(t, name: str):
         if inner != 1 and width > 1:
             raise ValueError(f"the values of a row of {name} must be adjacent")
         return rows, width, ld if rows > 1 else width
-    if len(shape) < 1 or not t.is_contiguous():
-        raise ValueError(f"{name} must be rows: two axes, or contiguous")
+    if len(shape) < 1:
+        raise ValueError(f"{name} must have rows")
     width = shape[-1]
-    return (t.numel() // width if width else 0), width, width
+    if t.is_contiguous():
+        return (t.numel() // width if width else 0), width, width
+    try:
+        return _rows_of(t.view(-1, width), name)
+    except RuntimeError:
+        raise ValueError(f"the rows of {name} must lie at one stride") from None
+
+
+def _q8_code(t, name: str) -> int:
+    code = _q8_codes.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype} of {name}")
+    return code
 
 
 def _q8_stride(t, name: str, shape, dtype, like) -> int:
@@ -452,7 +466,7 @@ def _q8_vector(t, name: str, n: int, like) -> int:
 def _q8_scales(x, scales, rows: int):
     """(scales of x's rows, pointer): the caller's or new ones."""
     if scales is None:
-        scales = x.new_empty(x.shape[:-1], dtype=_torch.float32)
+        scales = x.new_empty_strided((rows,), (1,), dtype=_torch.float32) if x.dim() == 2 else x.new_empty(x.shape[:-1], dtype=_torch.float32)
         return scales, scales.data_ptr()
     if scales.shape != x.shape[:-1]:
         raise ValueError(f"scales must have the shape {tuple(x.shape[:-1])}")
@@ -460,7 +474,20 @@ def _q8_scales(x, scales, rows: int):
 
 
 def _q8_like(x, dtype):
+    """A new tensor of x's shape, contiguous."""
+    if x.is_contiguous():
+        return _torch.empty_like(x, dtype=dtype)
     return _torch.empty_like(x, dtype=dtype, memory_format=_torch.contiguous_format)
+
+
+def _q8_new(x, rows: int, width: int):
+    """(new 8-bit rows for x, their stride): the rows start at multiples of 16 bytes, where nm_linear_q8 reads them in place."""
+    if width % 16 == 0 or rows == 1:
+        return _q8_like(x, _torch.int8), width
+    ld = (width + 15) // 16 * 16
+    if x.dim() == 2:
+        return x.new_empty_strided((rows, width), (ld, 1), dtype=_torch.int8), ld
+    return x.new_empty(x.shape[:-1] + (ld,), dtype=_torch.int8)[..., :width], ld
 
 
 def _q8_stream() -> int:
@@ -468,19 +495,19 @@ def _q8_stream() -> int:
 
 
 def nm_quantize_q8(x, q=None, scales=None, stream=None):
-    """Rows of x (fp32 or bf16, the last axis) rounded to 8 bits: (q int8 like x, scales fp32 [rows...]) with x ~ q * scales."""
+    """Rows of x (fp32 or bf16, the last axis) rounded to 8 bits: (q int8 like x, scales fp32 [rows...]) with x ~ q * scales.
+    A new q of an odd width has gaps between its rows."""
     L = _lib or lib()
     if stream is not None:
         with _torch.cuda.stream(stream):
             return nm_quantize_q8(x, q, scales)
     rows, width, ld = _rows_of(x, "x")
-    ldq = width
     if q is None:
-        q = _q8_like(x, _torch.int8)
+        q, ldq = _q8_new(x, rows, width)
     else:
         ldq = _q8_stride(q, "q", x.shape, _torch.int8, x)
     scales, sptr = _q8_scales(x, scales, rows)
-    rc = L.nm_quantize_q8(x.data_ptr(), _dtype_code(x), rows, width, ld, q.data_ptr(), ldq, sptr, _q8_stream())
+    rc = L.nm_quantize_q8(x.data_ptr(), _q8_code(x, "x"), rows, width, ld, q.data_ptr(), ldq, sptr, _q8_stream())
     if rc < 0:
         _check(rc)
     return q, scales
@@ -500,7 +527,7 @@ def nm_dequantize_q8(q, scales, dtype=None, y=None, stream=None):
         y = _q8_like(q, dtype or _torch.float32)
     else:
         ldy = _q8_stride(y, "y", q.shape, dtype or y.dtype, q)
-    rc = L.nm_dequantize_q8(q.data_ptr(), ld, _q8_vector(scales, "scales", rows, q), rows, width, y.data_ptr(), _dtype_code(y), ldy,
+    rc = L.nm_dequantize_q8(q.data_ptr(), ld, _q8_vector(scales, "scales", rows, q), rows, width, y.data_ptr(), _q8_code(y, "y"), ldy,
                             _q8_stream())
     if rc < 0:
         _check(rc)
@@ -509,7 +536,8 @@ def nm_dequantize_q8(q, scales, dtype=None, y=None, stream=None):
 
 def nm_rmsnorm_q8(x, gamma=None, residual=None, eps: float = 1e-6, q=None, scales=None, residual_out=None, stream=None):
     """h = x + residual; rows of gamma * h / sqrt(mean(h^2) + eps) rounded to 8 bits.  Returns (q, scales, h rounded to x's
-    dtype); the last is None without a residual unless residual_out is given.  residual_out may be x or residual."""
+    dtype); the last is None without a residual unless residual_out is given.  residual_out may be x or residual.  A new q of
+    an odd width has gaps between its rows."""
     L = _lib or lib()
     if stream is not None:
         with _torch.cuda.stream(stream):
@@ -517,7 +545,7 @@ def nm_rmsnorm_q8(x, gamma=None, residual=None, eps: float = 1e-6, q=None, scale
     rows, width, ld = _rows_of(x, "x")
     dtype = x.dtype
     ldr = rptr = optr = 0
-    ldq = ldo = width
+    ldo = width
     if residual is not None:
         ldr, rptr = _q8_stride(residual, "residual", x.shape, dtype, x), residual.data_ptr()
     if residual_out is not None:
@@ -526,11 +554,11 @@ def nm_rmsnorm_q8(x, gamma=None, residual=None, eps: float = 1e-6, q=None, scale
         residual_out = _q8_like(x, dtype)
         optr = residual_out.data_ptr()
     if q is None:
-        q = _q8_like(x, _torch.int8)
+        q, ldq = _q8_new(x, rows, width)
     else:
         ldq = _q8_stride(q, "q", x.shape, _torch.int8, x)
     scales, sptr = _q8_scales(x, scales, rows)
-    rc = L.nm_rmsnorm_q8(x.data_ptr(), _dtype_code(x), rows, width, ld, rptr, ldr,
+    rc = L.nm_rmsnorm_q8(x.data_ptr(), _q8_code(x, "x"), rows, width, ld, rptr, ldr,
                          0 if gamma is None else _q8_vector(gamma, "gamma", width, x), eps, optr, ldo, q.data_ptr(), ldq, sptr,
                          _q8_stream())
     if rc < 0:
@@ -570,7 +598,7 @@ def nm_q8_pack(w, scales=None, gated: bool = False, stream=None) -> Q8Weights:
         raise ValueError("w must have two axes")
     channels, width, ld = _rows_of(w, "w")
     sptr = 0 if scales is None else _q8_vector(scales, "scales", channels, w)
-    code = NM_I8 if w.dtype == _torch.int8 else _dtype_code(w)
+    code = _q8_code(w, "w")
     h = ctypes.c_void_p()
     _check(L.nm_q8_pack(w.data_ptr(), code, sptr, channels, width, ld, int(bool(gated)), _q8_stream(), ctypes.byref(h)))
     return Q8Weights(h, channels, width, bool(gated))
@@ -604,16 +632,18 @@ def nm_linear_q8(q, scales, w: Q8Weights, bias=None, residual=None, dtype=None, 
     if residual is not None:
         ldr, rptr = _q8_stride(residual, "residual", shape, y.dtype, q), residual.data_ptr()
     qptr = q.data_ptr()
-    need = ctypes.c_size_t(0)
-    rc = L.nm_linear_q8_workspace(qptr, rows, ld, w.handle, ctypes.byref(need))
-    if rc < 0:
-        _check(rc)
-    wptr, nbytes = None, need.value
-    if nbytes:
-        ws = q.new_empty(nbytes)
-        wptr = ws.data_ptr()
+    wptr, nbytes = None, 0
+    if rows > NM_Q8_FEW_ROWS or qptr % 16 or (rows > 1 and ld % 16):   # (else none is needed)
+        need = ctypes.c_size_t(0)
+        rc = L.nm_linear_q8_workspace(qptr, rows, ld, w.handle, ctypes.byref(need))
+        if rc < 0:
+            _check(rc)
+        nbytes = need.value
+        if nbytes:
+            ws = q.new_empty(nbytes)
+            wptr = ws.data_ptr()
     rc = L.nm_linear_q8(qptr, rows, width, ld, _q8_vector(scales, "scales", rows, q), w.handle,
-                        0 if bias is None else _q8_vector(bias, "bias", w.channels, q), rptr, ldr, y.data_ptr(), _dtype_code(y), ldy,
+                        0 if bias is None else _q8_vector(bias, "bias", w.channels, q), rptr, ldr, y.data_ptr(), _q8_code(y, "y"), ldy,
                         wptr, nbytes, _q8_stream())
     if rc < 0:
         _check(rc)

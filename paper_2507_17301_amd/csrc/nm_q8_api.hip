@@ -9,7 +9,7 @@ using namespace nm;
 
 namespace {
 
-constexpr int64_t kMaxRows = 0x7fffffff, kMaxStride = 1 << 24;
+constexpr int64_t kMaxRows = 1 << 30, kMaxStride = 1 << 24;
 
 inline size_t q8_elem(nm_dtype_t dt) { return dt == NM_F32 ? 4 : dt == NM_BF16 ? 2 : 1; }
 inline bool float_dtype(nm_dtype_t dt) { return dt == NM_F32 || dt == NM_BF16; }

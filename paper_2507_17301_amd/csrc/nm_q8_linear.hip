@@ -157,6 +157,23 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
     auto read = [&](int h, int i, unsigned at) {
         f[h][i] = *reinterpret_cast<const i32x4*>(smem + at + (i < 4 ? wlane + h * 4096 + i * 1024 : (qlane ^ (h * 64)) + (i - 4) * 2048));
     };
+    constexpr bool EARLY = !SPLIT && TB < 8;   // the scales come with the first stages where the registers last for it
+    Channels<GATED, 4> ch;
+    const int group = g0 + wr < p.groups ? g0 + wr : p.groups - 1;   // (what a wavefront past the last group has is not stored)
+    float early[EARLY ? TB : 1];
+    auto scale_of = [&](int j) {
+        const int64_t row = row0 + (wt * TB + j) * 16 + (lane & 15);
+        return row < p.rows ? p.qs[row] : 0.0f;
+    };
+    if constexpr (EARLY) {
+        ch.load(p, group, 0, lane);
+#pragma unroll
+        for (int j = 0; j < TB; ++j) early[j] = scale_of(j);
+    }
+    auto scale = [&](int j) {
+        if constexpr (EARLY) return early[j];
+        else return scale_of(j);
+    };
     i32x4 acc[TB][4] = {};
 #pragma unroll
     for (int s = 0; s < NS; ++s)
@@ -202,14 +219,12 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
 #pragma unroll
                 for (int b = 0; b < 4; ++b) to[(j * 4 + b) * 64] = acc[j][b];
     } else {
-        const int group = g0 + wr < p.groups ? g0 + wr : p.groups - 1;   // (what a wavefront past the last group has is not stored)
-        Channels<GATED, 4> ch;
-        ch.load(p, group, 0, lane);
+        if constexpr (!EARLY) ch.load(p, group, 0, lane);
         constexpr int kFit = T::kLds / (16 * WT * 64 * WR * 4 / (GATED ? 2 : 1));   // blocks of rows that fit LDS in fp32
         constexpr int JP4 = kFit >= TB ? TB : kFit >= TB / 2 ? TB / 2 : TB / 4, JP2 = 2 * kFit >= TB ? TB : TB / 2;
         static_assert(JP4 <= kFit && JP2 <= 2 * kFit, "the tile's outputs go through LDS");
-        if (!BF16 || p.res) store_tile<WR, WT, TB, JP4, true, GATED, BF16>(p, ch, acc, smem, wr, wt, lane, g0, row0);
-        else store_tile<WR, WT, TB, JP2, false, GATED, BF16>(p, ch, acc, smem, wr, wt, lane, g0, row0);
+        if (!BF16 || p.res) store_tile<WR, WT, TB, JP4, true, GATED, BF16>(p, ch, scale, acc, smem, wr, wt, lane, g0, row0);
+        else store_tile<WR, WT, TB, JP2, false, GATED, BF16>(p, ch, scale, acc, smem, wr, wt, lane, g0, row0);
     }
 }
 
@@ -244,7 +259,7 @@ __global__ __launch_bounds__(256) void q8_align_kernel(const int8_t* q, int64_t 
     const int c = (blockIdx.x * 256 + threadIdx.x) * 16;
     if (c >= pitch) return;
     for (int64_t row = blockIdx.y; row < rows; row += gridDim.y)
-        *reinterpret_cast<i32x4*>(to + row * pitch + c) = load16(q + row * ldq + c, width - c);
+        *reinterpret_cast<i32x4*>(to + row * pitch + c) = load16(q + row * ldq, c, width);
 }
 
 // ---------------------------------------------------------------- weights
@@ -259,7 +274,7 @@ __global__ __launch_bounds__(256) void q8_pack_kernel(const int8_t* w, int64_t l
         const int kb = (int)(gk % kblocks), group = (int)(gk / kblocks);
         const int c = q8_row_of(group * 64 + b * 16 + (lane & 15), channels, gated);
         const int k = kb * 64 + (lane >> 4) * 16;
-        *reinterpret_cast<i32x4*>(to + i * 16) = load16(w + (int64_t)c * ldw + k, c < 0 ? 0 : width - k);
+        *reinterpret_cast<i32x4*>(to + i * 16) = load16(w + (int64_t)(c < 0 ? 0 : c) * ldw, k, c < 0 ? 0 : width);
         if (kb == 0 && (lane >> 4) == 0) {
             const float s = c >= 0 ? scales[c] : 0.0f;
             if (!(fabsf(s) < INFINITY)) atomicOr(bad, 1);
@@ -287,7 +302,7 @@ __global__ __launch_bounds__(256) void q8_unpack_kernel(const int8_t* from, cons
 __global__ void q8_clear_kernel(int* p) { *p = 0; }
 
 // ---------------------------------------------------------------- launches
-constexpr int kFewRows = 64;
+constexpr int kFewRows = NM_Q8_FEW_ROWS;
 
 // Whether the kernels can read q where it lies.
 inline bool aligned16(const Q8Linear& p) { return (uintptr_t)p.q % 16 == 0 && (p.rows == 1 || p.ldq % 16 == 0); }

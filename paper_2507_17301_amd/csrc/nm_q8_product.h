@@ -26,15 +26,20 @@ __device__ inline i32x4 mma(i32x4 w, i32x4 q, i32x4 acc) { return __builtin_amdg
 // of its last value, and so its page.
 __device__ inline unsigned rows_extent(const Q8Linear& p, int rows) { return (unsigned)((rows - 1) * p.ldq + ((p.width + 15) & ~15)); }
 
-// The first n (1 to 16; all for more, none for less) of 16 bytes at any address, zeros after them.
-__device__ inline i32x4 load16(const int8_t* p, int n)
+// 16 bytes of a row from byte c on, zeros past its end; the row may begin at any address.
+__device__ inline i32x4 load16(const int8_t* row, int c, int width)
 {
     i32x4 v = {0, 0, 0, 0};
-    if (n >= 16) {
-        __builtin_memcpy(&v, p, 16);
+    if (c + 16 <= width) {
+        __builtin_memcpy(&v, row + c, 16);
+    } else if (c < width && width >= 16) {   // the row's last 16, moved down to where its end is
+        unsigned __int128 u;
+        __builtin_memcpy(&u, row + width - 16, 16);
+        u >>= 8 * (c + 16 - width);
+        __builtin_memcpy(&v, &u, 16);
     } else {
-        for (int e = 0; e < n; ++e) {
-            const int b = (int)(unsigned char)p[e] << (8 * (e & 3));
+        for (int e = 0; c + e < width; ++e) {
+            const int b = (int)(unsigned char)row[c + e] << (8 * (e & 3));
 #pragma unroll
             for (int d = 0; d < 4; ++d) v[d] |= (e >> 2) == d ? b : 0;
         }
@@ -146,9 +151,9 @@ __device__ inline void emit(const Q8Linear& p, const Channels<GATED, NB>& ch, co
 // straight from the registers (above) a store instruction reaches 16 rows with 64 bytes each, and 8192 x 4096 -> 16384 took 433 us
 // instead of 422, 8000 x 2000 -> 5000 (rows that begin in the middle of a line) 99 instead of 92.  JP of the TB blocks of rows at a time, STAGE32 in fp32 (for a residual, so that it rounds once).
 // The 16-byte pieces of a row lie at piece ^ (row & 7).
-template <int WR, int WT, int TB, int JP, bool STAGE32, bool GATED, bool BF16>
-__device__ inline void store_tile(const Q8Linear& p, const Channels<GATED, 4>& ch, const i32x4 (&acc)[TB][4], char* smem, int wr, int wt, int lane,
-                                  int group0, int64_t row0)
+template <int WR, int WT, int TB, int JP, bool STAGE32, bool GATED, bool BF16, typename Scale>
+__device__ inline void store_tile(const Q8Linear& p, const Channels<GATED, 4>& ch, Scale scale, const i32x4 (&acc)[TB][4], char* smem,
+                                  int wr, int wt, int lane, int group0, int64_t row0)
 {
     constexpr int SB = STAGE32 ? 4 : 2, ES = Elem<BF16>::kBytes, C = Channels<GATED, 4>::kRuns * 8;   // outputs of a group and lane
     constexpr int kOuts = WR * C * 4, kPitch = kOuts * SB, kThreads = WR * WT * 64, kRows = WT * JP * 16;
@@ -159,9 +164,8 @@ __device__ inline void store_tile(const Q8Linear& p, const Channels<GATED, 4>& c
         __syncthreads();   // the stages, or the outputs before, have been read
 #pragma unroll
         for (int jj = 0; jj < JP; ++jj) {
-            const int64_t row = row0 + (wt * TB + j0 + jj) * 16 + (lane & 15);
-            const float s = row < p.rows ? p.qs[row] : 0.0f;
             const int lrow = (wt * JP + jj) * 16 + (lane & 15);
+            const float s = scale(j0 + jj);
 #pragma unroll
             for (int run = 0; run < Channels<GATED, 4>::kRuns; ++run) {
                 float y[8];

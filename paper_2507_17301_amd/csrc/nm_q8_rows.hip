@@ -5,7 +5,7 @@
 // Bound by HBM: a value is read once (twice with a residual), kept in registers over both reductions (sum of
 // squares, largest magnitude), and written once.  NT threads share a row, 8 adjacent values a thread at a time,
 // so that a wavefront reads 1 KiB (bf16) or 2 KiB (fp32) of adjacent bytes an instruction and writes 512 bytes
-// of q.  One wavefront a row up to 1024 values (no barrier), 256 threads up to 16384, 1024 beyond.
+// of q.  One wavefront a row up to 1024 values (no barrier), a workgroup beyond (pick_rows).
 // Rows of odd widths and strides run the same code (global memory takes a 16-byte access at any address); only what a width leaves past its last group of 8 is
 // taken value by value, one value a thread.
 #include "nm_q8_device.h"
@@ -54,6 +54,7 @@ template <bool BF16, int NT, int VPT, bool NORM>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
 {
     constexpr int ES = Elem<BF16>::kBytes, BLOCK = NT < 256 ? 256 : NT, RPB = BLOCK / NT;
+    constexpr bool EARLY = VPT <= 2;
     __shared__ float psum[NT / 64];
     __shared__ unsigned pmax[NT / 64];
     const int t = threadIdx.x % NT;
@@ -97,6 +98,15 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
         }
         bool bad = false;
         if constexpr (NORM) {
+            float gain[EARLY ? VPT : 1][8], gx = 1.0f;   // (read ahead of the reductions, while the registers last)
+            if (EARLY && p.gamma) {
+#pragma unroll
+                for (int v = 0; v < VPT; ++v) {
+                    const int c = (v * NT + t) * 8;
+                    if (c < whole) Elem<false>::load8((const char*)(p.gamma + c), gain[v]);
+                }
+                if (t < over) gx = p.gamma[whole + t];
+            }
             float sum = hx * hx;
 #pragma unroll
             for (int v = 0; v < VPT; ++v)
@@ -115,13 +125,15 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
                 for (int v = 0; v < VPT; ++v) {
                     const int c = (v * NT + t) * 8;
                     if (c < whole) {
-                        float g[8];
-                        Elem<false>::load8((const char*)(p.gamma + c), g);
+                        if constexpr (!EARLY) Elem<false>::load8((const char*)(p.gamma + c), gain[0]);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) h[v][e] *= g[e];
+                        for (int e = 0; e < 8; ++e) h[v][e] *= gain[EARLY ? v : 0][e];
                     }
                 }
-                if (t < over) hx *= p.gamma[whole + t];
+                if constexpr (!EARLY) {
+                    if (t < over) gx = p.gamma[whole + t];
+                }
+                hx *= gx;
             }
         }
         // the largest magnitude as bits: a NaN is larger than infinity, which is larger than any number
@@ -161,7 +173,7 @@ __global__ __launch_bounds__(256) void q8_dequantize_kernel(const int8_t* q, int
     constexpr int ES = Elem<BF16>::kBytes;
     const int64_t total = rows * units;   // of 8 values
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / units;
+        const int64_t row = total <= 0xffffffffll ? (int64_t)((unsigned)i / (unsigned)units) : i / units;
         const int c = (int)(i - row * units) * 8;
         const int8_t* pq = q + row * ldq + c;
         char* py = y + (row * ldy + c) * ES;
@@ -179,32 +191,38 @@ __global__ __launch_bounds__(256) void q8_dequantize_kernel(const int8_t* q, int
     }
 }
 
-template <bool BF16, int NT, int VPT>
-int launch_rows(const RowArgs& p, bool norm, hipStream_t s)
+template <bool BF16, int NT, int VPT, bool NORM>
+int launch_rows(const RowArgs& p, hipStream_t s)
 {
     constexpr int BLOCK = NT < 256 ? 256 : NT, RPB = BLOCK / NT;
     const int64_t blocks = (p.rows + RPB - 1) / RPB;
     const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
-    if (norm)
-        hipLaunchKernelGGL((q8_rows_kernel<BF16, NT, VPT, true>), dim3(grid), dim3(BLOCK), 0, s, p);
-    else
-        hipLaunchKernelGGL((q8_rows_kernel<BF16, NT, VPT, false>), dim3(grid), dim3(BLOCK), 0, s, p);
+    hipLaunchKernelGGL((q8_rows_kernel<BF16, NT, VPT, NORM>), dim3(grid), dim3(BLOCK), 0, s, p);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }
 
-template <bool BF16>
-int pick_rows(const RowArgs& p, bool norm, hipStream_t s)
+// Threads of a row.  us, bf16, threads x groups of 8 a thread, 1 row and 16384:
+//   norm      4096   512 x 1  3.2   91     256 x 2  3.6   92     256 x 4  4.1  126    1024 x 1  3.5  134
+//             8192  1024 x 1  4.0  189     512 x 2  3.8  195     256 x 4  5.1  224     512 x 4  4.4  345
+//            16384  1024 x 2  4.9  342     256 x 8  7.1  392     512 x 4  5.5  566
+//   rounding  4096   256 x 2  2.6   37     512 x 1  2.6   39    1024 x 1  2.7   65
+//             8192   512 x 2  2.6   69     256 x 4  2.9   73    1024 x 1  2.7   84
+//            16384  1024 x 2  3.0  134     256 x 8  3.9  144     512 x 4  3.1  145
+// (16384 rows: 5.0 to 5.4 TB/s for the norm, 5.5 to 6.0 for the rounding, whose rows partly come from the last-level cache.)
+template <bool BF16, bool NORM>
+int pick_rows(const RowArgs& p, hipStream_t s)
 {
     const int w = p.width;
-    if (w <= 512) return launch_rows<BF16, 64, 1>(p, norm, s);
-    if (w <= 1024) return launch_rows<BF16, 64, 2>(p, norm, s);
-    if (w <= 2048) return launch_rows<BF16, 256, 1>(p, norm, s);
-    if (w <= 4096) return launch_rows<BF16, 256, 2>(p, norm, s);
-    if (w <= 8192) return launch_rows<BF16, 256, 4>(p, norm, s);
-    if (w <= 16384) return launch_rows<BF16, 256, 8>(p, norm, s);
-    if (w <= 32768) return launch_rows<BF16, 1024, 4>(p, norm, s);
-    return launch_rows<BF16, 1024, 8>(p, norm, s);
+    if (w <= 512) return launch_rows<BF16, 64, 1, NORM>(p, s);
+    if (w <= 1024) return launch_rows<BF16, 64, 2, NORM>(p, s);
+    if (w <= 2048) return launch_rows<BF16, 256, 1, NORM>(p, s);
+    if (w <= 4096) return launch_rows<BF16, NORM ? 512 : 256, NORM ? 1 : 2, NORM>(p, s);
+    if (w <= 6144 || (w <= 8192 && !NORM)) return launch_rows<BF16, 512, 2, NORM>(p, s);   // (1024 threads would not all have work)
+    if (w <= 8192) return launch_rows<BF16, 1024, 1, NORM>(p, s);
+    if (w <= 16384) return launch_rows<BF16, 1024, 2, NORM>(p, s);
+    if (w <= 32768) return launch_rows<BF16, 1024, 4, NORM>(p, s);
+    return launch_rows<BF16, 1024, 8, NORM>(p, s);
 }
 
 }  // namespace
@@ -214,7 +232,8 @@ int run_q8_rows(const void* x, nm_dtype_t dt, int64_t rows, int width, int64_t l
                 hipStream_t s)
 {
     RowArgs p{(const char*)x, (const char*)res, gamma, (char*)out, q, scales, rows, ldx, ldr, ldo, ldq, width, eps};
-    return dt == NM_F32 ? pick_rows<false>(p, norm, s) : pick_rows<true>(p, norm, s);
+    if (dt == NM_F32) return norm ? pick_rows<false, true>(p, s) : pick_rows<false, false>(p, s);
+    return norm ? pick_rows<true, true>(p, s) : pick_rows<true, false>(p, s);
 }
 
 int run_q8_dequantize(const int8_t* q, int64_t ldq, const float* scales, int64_t rows, int width, void* y, nm_dtype_t dt,
