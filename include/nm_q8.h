@@ -126,6 +126,45 @@ int nm_linear_q8(const int8_t* q_dev, int64_t rows, int width, int64_t ldq, cons
 enum { NM_Q8_FEW_ROWS = 64 };
 int nm_linear_q8_workspace(const int8_t* q_dev, int64_t rows, int64_t ldq, const nm_q8_t* w, size_t* bytes);
 
+/*
+ * The calls above with their arguments in one block, for bindings that pay for every argument (as nm_conv2d_args).  dtype is
+ * x_dtype or y_dtype.  norm = 0 is nm_quantize_q8, which looks at neither residual, gamma, eps nor residual_out.
+ */
+typedef struct nm_rows_q8_args {
+    const void* x_dev;
+    const void* residual_dev;
+    const float* gamma_dev;
+    void* residual_out_dev;
+    int8_t* q_dev;
+    float* scales_dev;
+    void* hip_stream;
+    int64_t dtype, rows, width, ldx, ldr, ldo, ldq, norm;
+    double eps;
+} nm_rows_q8_args_t;
+int nm_rows_q8_args(const nm_rows_q8_args_t* args);
+
+typedef struct nm_dequantize_q8_args {
+    const int8_t* q_dev;
+    const float* scales_dev;
+    void* y_dev;
+    void* hip_stream;
+    int64_t dtype, rows, width, ldq, ldy;
+} nm_dequantize_q8_args_t;
+int nm_dequantize_q8_args(const nm_dequantize_q8_args_t* args);
+
+typedef struct nm_linear_q8_args {
+    const int8_t* q_dev;
+    const float* scales_dev;
+    const nm_q8_t* w;
+    const float* bias_dev;
+    const void* residual_dev;
+    void* y_dev;
+    void* workspace_dev;
+    void* hip_stream;
+    int64_t dtype, rows, width, ldq, ldr, ldy, workspace_bytes;
+} nm_linear_q8_args_t;
+int nm_linear_q8_args(const nm_linear_q8_args_t* args);
+
 #ifdef __cplusplus
 }
 #endif

@@ -88,6 +88,7 @@ def lib():
         L.nm_q8_dims.argtypes = [vp, pi, pi, pi]
         L.nm_q8_export.argtypes = [vp, vp, vp]
         L.nm_linear_q8.argtypes = [vp, i64, ci, i64, vp, vp, vp, vp, i64, vp, ci, i64, vp, st, vp]
+        L.nm_rows_q8_args.argtypes = L.nm_dequantize_q8_args.argtypes = L.nm_linear_q8_args.argtypes = [ctypes.c_char_p]
         L.nm_linear_q8_workspace.argtypes = [vp, i64, i64, vp, ctypes.POINTER(st)]
         for name in ("nm_prune", "nm_packed_free", "nm_packed_dims", "nm_packed_indices",
                      "nm_packed_values", "nm_packed_mask", "nm_packed_scale", "nm_conv2d", "nm_conv2d_res", "nm_conv2d_static", "nm_conv2d_args",
@@ -95,10 +96,16 @@ def lib():
                      "nm_avgpool_global", "nm_im2col", "nm_stream_floor", "nm_autotune",
                      "nm_cache_save", "nm_cache_load", "nm_cache_clear", "nm_cache_size", "nm_workspace_free",
                      "nm_force_variant", "nm_variant_legal", "nm_quantize_q8", "nm_dequantize_q8", "nm_rmsnorm_q8",
-                     "nm_q8_pack", "nm_q8_free", "nm_q8_dims", "nm_q8_export", "nm_linear_q8", "nm_linear_q8_workspace"):
+                     "nm_q8_pack", "nm_q8_free", "nm_q8_dims", "nm_q8_export", "nm_linear_q8", "nm_linear_q8_workspace", "nm_rows_q8_args",
+                     "nm_dequantize_q8_args", "nm_linear_q8_args"):
             getattr(L, name).restype = ci
         _lib = L
     return _lib
+
+
+def _lib_torch():
+    lib()
+    return _torch
 
 
 def _check(rc: int) -> int:
@@ -442,35 +449,25 @@ def _rows_of(t, name: str):
         raise ValueError(f"the rows of {name} must lie at one stride") from None
 
 
-def _q8_code(t, name: str) -> int:
-    code = _q8_codes.get(t.dtype)
+def _q8_code(dtype, name: str) -> int:
+    code = _q8_codes.get(dtype)
     if code is None:
-        raise TypeError(f"unsupported dtype {t.dtype} of {name}")
+        raise TypeError(f"unsupported dtype {dtype} of {name}")
     return code
 
 
-def _q8_stride(t, name: str, shape, dtype, like) -> int:
-    """Row stride of a tensor that the caller gave and that has to have this shape and type."""
-    if t.shape != shape or t.dtype != dtype or t.get_device() != like.get_device():
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {like.device}")
+def _q8_stride(t, name: str, shape, dtype, dev: int) -> int:
+    """Row stride of a tensor that the caller gave and that has to have this shape and type, on device `dev`."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on device {dev}")
     return _rows_of(t, name)[2]
 
 
-def _q8_vector(t, name: str, n: int, like) -> int:
-    """Pointer of a contiguous fp32 vector of n values on the device of `like`."""
-    if t.dtype != _torch.float32 or t.numel() != n or t.get_device() != like.get_device() or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous fp32 tensor of {n} values on {like.device}")
+def _q8_vector(t, name: str, n: int, dev: int) -> int:
+    """Pointer of a contiguous fp32 vector of n values on device `dev`."""
+    if t.dtype != _torch.float32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous fp32 tensor of {n} values on device {dev}")
     return t.data_ptr()
-
-
-def _q8_scales(x, scales, rows: int):
-    """(scales of x's rows, pointer): the caller's or new ones."""
-    if scales is None:
-        scales = x.new_empty_strided((rows,), (1,), dtype=_torch.float32) if x.dim() == 2 else x.new_empty(x.shape[:-1], dtype=_torch.float32)
-        return scales, scales.data_ptr()
-    if scales.shape != x.shape[:-1]:
-        raise ValueError(f"scales must have the shape {tuple(x.shape[:-1])}")
-    return scales, _q8_vector(scales, "scales", rows, x)
 
 
 def _q8_like(x, dtype):
@@ -494,76 +491,85 @@ def _q8_stream() -> int:
     return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice())
 
 
-def nm_quantize_q8(x, q=None, scales=None, stream=None):
-    """Rows of x (fp32 or bf16, the last axis) rounded to 8 bits: (q int8 like x, scales fp32 [rows...]) with x ~ q * scales.
-    A new q of an odd width has gaps between its rows."""
+_ROWS_ARGS = struct.Struct("15qd")       # nm_rows_q8_args_t
+_DEQUANTIZE_ARGS = struct.Struct("9q")   # nm_dequantize_q8_args_t
+_LINEAR_ARGS = struct.Struct("15q")      # nm_linear_q8_args_t
+
+
+def _q8_rows(norm: bool, x, gamma, residual, eps, q, scales, residual_out):
     L = _lib or lib()
-    if stream is not None:
-        with _torch.cuda.stream(stream):
-            return nm_quantize_q8(x, q, scales)
     rows, width, ld = _rows_of(x, "x")
-    if q is None:
-        q, ldq = _q8_new(x, rows, width)
-    else:
-        ldq = _q8_stride(q, "q", x.shape, _torch.int8, x)
-    scales, sptr = _q8_scales(x, scales, rows)
-    rc = L.nm_quantize_q8(x.data_ptr(), _q8_code(x, "x"), rows, width, ld, q.data_ptr(), ldq, sptr, _q8_stream())
-    if rc < 0:
-        _check(rc)
-    return q, scales
-
-
-def nm_dequantize_q8(q, scales, dtype=None, y=None, stream=None):
-    """The values that 8-bit rows stand for, q * scales, in fp32 or bf16 (`dtype`; default fp32 or y's)."""
-    L = _lib or lib()
-    if stream is not None:
-        with _torch.cuda.stream(stream):
-            return nm_dequantize_q8(q, scales, dtype, y)
-    rows, width, ld = _rows_of(q, "q")
-    if q.dtype != _torch.int8:
-        raise TypeError(f"q must be int8, not {q.dtype}")
-    ldy = width
-    if y is None:
-        y = _q8_like(q, dtype or _torch.float32)
-    else:
-        ldy = _q8_stride(y, "y", q.shape, dtype or y.dtype, q)
-    rc = L.nm_dequantize_q8(q.data_ptr(), ld, _q8_vector(scales, "scales", rows, q), rows, width, y.data_ptr(), _q8_code(y, "y"), ldy,
-                            _q8_stream())
-    if rc < 0:
-        _check(rc)
-    return y
-
-
-def nm_rmsnorm_q8(x, gamma=None, residual=None, eps: float = 1e-6, q=None, scales=None, residual_out=None, stream=None):
-    """h = x + residual; rows of gamma * h / sqrt(mean(h^2) + eps) rounded to 8 bits.  Returns (q, scales, h rounded to x's
-    dtype); the last is None without a residual unless residual_out is given.  residual_out may be x or residual.  A new q of
-    an odd width has gaps between its rows."""
-    L = _lib or lib()
-    if stream is not None:
-        with _torch.cuda.stream(stream):
-            return nm_rmsnorm_q8(x, gamma, residual, eps, q, scales, residual_out)
-    rows, width, ld = _rows_of(x, "x")
-    dtype = x.dtype
-    ldr = rptr = optr = 0
+    dtype, dev = x.dtype, x.get_device()
+    code = _q8_code(dtype, "x")
+    gptr = rptr = optr = ldr = 0
     ldo = width
+    if gamma is not None:
+        gptr = _q8_vector(gamma, "gamma", width, dev)
     if residual is not None:
-        ldr, rptr = _q8_stride(residual, "residual", x.shape, dtype, x), residual.data_ptr()
+        ldr, rptr = _q8_stride(residual, "residual", x.shape, dtype, dev), residual.data_ptr()
     if residual_out is not None:
-        ldo, optr = _q8_stride(residual_out, "residual_out", x.shape, dtype, x), residual_out.data_ptr()
+        ldo, optr = _q8_stride(residual_out, "residual_out", x.shape, dtype, dev), residual_out.data_ptr()
     elif residual is not None:
         residual_out = _q8_like(x, dtype)
         optr = residual_out.data_ptr()
     if q is None:
         q, ldq = _q8_new(x, rows, width)
     else:
-        ldq = _q8_stride(q, "q", x.shape, _torch.int8, x)
-    scales, sptr = _q8_scales(x, scales, rows)
-    rc = L.nm_rmsnorm_q8(x.data_ptr(), _q8_code(x, "x"), rows, width, ld, rptr, ldr,
-                         0 if gamma is None else _q8_vector(gamma, "gamma", width, x), eps, optr, ldo, q.data_ptr(), ldq, sptr,
-                         _q8_stream())
+        ldq = _q8_stride(q, "q", x.shape, _torch.int8, dev)
+    if scales is None:
+        scales = x.new_empty_strided((rows,), (1,), dtype=_torch.float32) if x.dim() == 2 else x.new_empty(x.shape[:-1], dtype=_torch.float32)
+        sptr = scales.data_ptr()
+    else:
+        if scales.shape != x.shape[:-1]:
+            raise ValueError(f"scales must have the shape {tuple(x.shape[:-1])}")
+        sptr = _q8_vector(scales, "scales", rows, dev)
+    rc = L.nm_rows_q8_args(_ROWS_ARGS.pack(x.data_ptr(), rptr, gptr, optr, q.data_ptr(), sptr, _q8_stream(), code, rows, width, ld, ldr, ldo,
+                                           ldq, norm, eps))
     if rc < 0:
         _check(rc)
     return q, scales, residual_out
+
+
+def nm_quantize_q8(x, q=None, scales=None, stream=None):
+    """Rows of x (fp32 or bf16, the last axis) rounded to 8 bits: (q int8 like x, scales fp32 [rows...]) with x ~ q * scales.
+    A new q of an odd width has gaps between its rows."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return _q8_rows(False, x, None, None, 0.0, q, scales, None)[:2]
+    return _q8_rows(False, x, None, None, 0.0, q, scales, None)[:2]
+
+
+def nm_rmsnorm_q8(x, gamma=None, residual=None, eps: float = 1e-6, q=None, scales=None, residual_out=None, stream=None):
+    """h = x + residual; rows of gamma * h / sqrt(mean(h^2) + eps) rounded to 8 bits.  Returns (q, scales, h rounded to x's
+    dtype); the last is None without a residual unless residual_out is given.  residual_out may be x or residual.  A new q of
+    an odd width has gaps between its rows."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return _q8_rows(True, x, gamma, residual, eps, q, scales, residual_out)
+    return _q8_rows(True, x, gamma, residual, eps, q, scales, residual_out)
+
+
+def nm_dequantize_q8(q, scales, dtype=None, y=None, stream=None):
+    """The values that 8-bit rows stand for, q * scales, in fp32 or bf16 (`dtype`; default fp32 or y's)."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return nm_dequantize_q8(q, scales, dtype, y)
+    L = _lib or lib()
+    rows, width, ld = _rows_of(q, "q")
+    if q.dtype != _torch.int8:
+        raise TypeError(f"q must be int8, not {q.dtype}")
+    dev, ldy = q.get_device(), width
+    if y is None:
+        dtype = dtype or _torch.float32
+        y = _q8_like(q, dtype)
+    else:
+        dtype = dtype or y.dtype
+        ldy = _q8_stride(y, "y", q.shape, dtype, dev)
+    rc = L.nm_dequantize_q8_args(_DEQUANTIZE_ARGS.pack(q.data_ptr(), _q8_vector(scales, "scales", rows, dev), y.data_ptr(), _q8_stream(),
+                                                       _q8_code(dtype, "y"), rows, width, ld, ldy))
+    if rc < 0:
+        _check(rc)
+    return y
 
 
 class Q8Weights:
@@ -590,17 +596,16 @@ class Q8Weights:
 def nm_q8_pack(w, scales=None, gated: bool = False, stream=None) -> Q8Weights:
     """Weights [channels, width] on the device: int8 with fp32 scales [channels], or fp32 / bf16, which are rounded here
     (a scale for each channel).  gated: the first half of the channels gates the second."""
-    L = _lib or lib()
     if stream is not None:
-        with _torch.cuda.stream(stream):
+        with _lib_torch().cuda.stream(stream):
             return nm_q8_pack(w, scales, gated)
+    L = _lib or lib()
     if w.dim() != 2:
         raise ValueError("w must have two axes")
     channels, width, ld = _rows_of(w, "w")
-    sptr = 0 if scales is None else _q8_vector(scales, "scales", channels, w)
-    code = _q8_code(w, "w")
+    sptr = 0 if scales is None else _q8_vector(scales, "scales", channels, w.get_device())
     h = ctypes.c_void_p()
-    _check(L.nm_q8_pack(w.data_ptr(), code, sptr, channels, width, ld, int(bool(gated)), _q8_stream(), ctypes.byref(h)))
+    _check(L.nm_q8_pack(w.data_ptr(), _q8_code(w.dtype, "w"), sptr, channels, width, ld, int(bool(gated)), _q8_stream(), ctypes.byref(h)))
     return Q8Weights(h, channels, width, bool(gated))
 
 
@@ -615,36 +620,40 @@ def nm_linear_q8(q, scales, w: Q8Weights, bias=None, residual=None, dtype=None, 
     """8-bit rows times 8-bit weights: (q @ w.T) * scales * channel scales + bias + residual, or the gated form
     silu(gate) * up.  y: [..., channels] (gated: half of them) in bf16 (default) or fp32; residual is typed and shaped
     like y and may be y."""
-    L = _lib or lib()
     if stream is not None:
-        with _torch.cuda.stream(stream):
+        with _lib_torch().cuda.stream(stream):
             return nm_linear_q8(q, scales, w, bias, residual, dtype, y)
+    L = _lib or lib()
     rows, width, ld = _rows_of(q, "q")
     if q.dtype != _torch.int8:
         raise TypeError(f"q must be int8, not {q.dtype}")
-    shape = q.shape[:-1] + (w.outs,)
-    ldy = w.outs
+    dev, outs = q.get_device(), w.outs
+    shape = (rows, outs) if q.dim() == 2 else q.shape[:-1] + (outs,)
+    ldy = outs
     if y is None:
-        y = q.new_empty(shape, dtype=dtype or _torch.bfloat16)
+        dtype = dtype or _torch.bfloat16
+        y = q.new_empty(shape, dtype=dtype)
     else:
-        ldy = _q8_stride(y, "y", shape, dtype or y.dtype, q)
-    ldr = rptr = 0
+        dtype = dtype or y.dtype
+        ldy = _q8_stride(y, "y", shape, dtype, dev)
+    bptr = rptr = ldr = 0
+    if bias is not None:
+        bptr = _q8_vector(bias, "bias", w.channels, dev)
     if residual is not None:
-        ldr, rptr = _q8_stride(residual, "residual", shape, y.dtype, q), residual.data_ptr()
-    qptr = q.data_ptr()
-    wptr, nbytes = None, 0
+        ldr, rptr = _q8_stride(residual, "residual", shape, dtype, dev), residual.data_ptr()
+    qptr, handle = q.data_ptr(), w.handle.value if w.handle else 0
+    wptr = nbytes = 0
     if rows > NM_Q8_FEW_ROWS or qptr % 16 or (rows > 1 and ld % 16):   # (else none is needed)
         need = ctypes.c_size_t(0)
-        rc = L.nm_linear_q8_workspace(qptr, rows, ld, w.handle, ctypes.byref(need))
+        rc = L.nm_linear_q8_workspace(qptr, rows, ld, handle, ctypes.byref(need))
         if rc < 0:
             _check(rc)
         nbytes = need.value
         if nbytes:
             ws = q.new_empty(nbytes)
             wptr = ws.data_ptr()
-    rc = L.nm_linear_q8(qptr, rows, width, ld, _q8_vector(scales, "scales", rows, q), w.handle,
-                        0 if bias is None else _q8_vector(bias, "bias", w.channels, q), rptr, ldr, y.data_ptr(), _q8_code(y, "y"), ldy,
-                        wptr, nbytes, _q8_stream())
+    rc = L.nm_linear_q8_args(_LINEAR_ARGS.pack(qptr, _q8_vector(scales, "scales", rows, dev), handle, bptr, rptr, y.data_ptr(), wptr,
+                                               _q8_stream(), _q8_code(dtype, "y"), rows, width, ld, ldr, ldy, nbytes))
     if rc < 0:
         _check(rc)
     return y

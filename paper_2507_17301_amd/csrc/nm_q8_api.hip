@@ -403,4 +403,38 @@ int nm_linear_q8(const int8_t* q, int64_t rows, int width, int64_t ldq, const fl
     return run_q8_linear(p, workspace, (hipStream_t)stream);
 }
 
+// The integers of a block are 64 bits wide; one that does not fit an int is out of range for every argument that is one.
+static inline int narrow(int64_t v) { return v < -1 || v > 0x7fffffff ? -1 : (int)v; }
+
+int nm_rows_q8_args(const nm_rows_q8_args_t* a)
+{
+    if (!a) {
+        set_error("null pointer argument");
+        return NM_ERR_ARG;
+    }
+    if (a->norm)
+        return nm_rmsnorm_q8(a->x_dev, narrow(a->dtype), a->rows, narrow(a->width), a->ldx, a->residual_dev, a->ldr, a->gamma_dev, (float)a->eps,
+                             a->residual_out_dev, a->ldo, a->q_dev, a->ldq, a->scales_dev, a->hip_stream);
+    return nm_quantize_q8(a->x_dev, narrow(a->dtype), a->rows, narrow(a->width), a->ldx, a->q_dev, a->ldq, a->scales_dev, a->hip_stream);
+}
+
+int nm_dequantize_q8_args(const nm_dequantize_q8_args_t* a)
+{
+    if (!a) {
+        set_error("null pointer argument");
+        return NM_ERR_ARG;
+    }
+    return nm_dequantize_q8(a->q_dev, a->ldq, a->scales_dev, a->rows, narrow(a->width), a->y_dev, narrow(a->dtype), a->ldy, a->hip_stream);
+}
+
+int nm_linear_q8_args(const nm_linear_q8_args_t* a)
+{
+    if (!a) {
+        set_error("null pointer argument");
+        return NM_ERR_ARG;
+    }
+    return nm_linear_q8(a->q_dev, a->rows, narrow(a->width), a->ldq, a->scales_dev, a->w, a->bias_dev, a->residual_dev, a->ldr, a->y_dev,
+                        narrow(a->dtype), a->ldy, a->workspace_dev, a->workspace_bytes < 0 ? 0 : (size_t)a->workspace_bytes, a->hip_stream);
+}
+
 }  // extern "C"
