@@ -107,7 +107,7 @@ __global__ __launch_bounds__(NW * 64) void q8_few_kernel(Q8Linear p)
 // K goes by in steps of 128: both operands' next step is loaded straight into LDS while the present one is multiplied.
 // Weights lie in LDS as in memory (a wavefront's operand is 1 KiB of adjacent bytes); a row's 128 bytes are 8 chunks of 16,
 // chunk c stored at c ^ (row & 7), so that the 8 rows that an LDS cycle reads lie in 8 different places.
-// SPLIT: blockIdx.y takes `per` of the K steps and stores its integer sums as they lie in the registers,
+// SPLIT: a workgroup takes `per` of the K steps and stores its integer sums as they lie in the registers,
 //   part[split][tile][wave][16-row block][4 blocks][64 lanes], for q8_join_kernel to add and scale.
 template <int WR, int WT, int TB, int NS> struct Tile {
     static constexpr int kWaves = WR * WT, kRows = 16 * TB * WT;
@@ -123,13 +123,13 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wr = wave % WR, wt = wave / WR;
-    int tc, tr, tile;
-    if (!order.at(blockIdx.x, tc, tr, tile)) return;
+    int tc, tr, tile, split;
+    order.at(blockIdx.x, tc, tr, tile, split);
     const int g0 = tc * WR;
     const int64_t row0 = (int64_t)tr * T::kRows;
     const int nrow = (int)(p.rows - row0 < T::kRows ? p.rows - row0 : T::kRows);
     const int ngrp = p.groups - g0 < WR ? p.groups - g0 : WR;
-    const int first = SPLIT ? blockIdx.y * per : 0;
+    const int first = SPLIT ? split * per : 0;
     const int steps = SPLIT ? (p.kblocks / 2 - first < per ? p.kblocks / 2 - first : per) : p.kblocks / 2;
     const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + (size_t)g0 * p.kblocks * 4096, (unsigned)ngrp * p.kblocks * 4096);
     const __amdgpu_buffer_rsrc_t qsr = q8_rsrc(p.q + row0 * p.ldq, rows_extent(p, nrow));
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // no load into LDS outlives the workgroup
     if constexpr (SPLIT) {
         if (g0 + wr >= p.groups) return;
-        i32x4* to = part + ((size_t)(blockIdx.y * order.tiles_c * order.tiles_r + tile) * T::kWaves + wave) * TB * 256 + lane;
+        i32x4* to = part + ((size_t)((size_t)split * order.tiles() + tile) * T::kWaves + wave) * TB * 256 + lane;
 #pragma unroll
         for (int j = 0; j < TB; ++j)
             if (wt * TB * 16 + j * 16 < nrow)
@@ -230,26 +230,27 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
 
 // Adds the sums of `splits` parts and stores the results: a wavefront takes 16 rows x 64 packed channels.
 template <int WR, int WT, int TB, int NS, bool GATED, bool BF16>
-__global__ __launch_bounds__(256) void q8_join_kernel(Q8Linear p, TileOrder order, int splits, const i32x4* part)
+__global__ __launch_bounds__(256) void q8_join_kernel(Q8Linear p, TileOrder order, const i32x4* part)
 {
     using T = Tile<WR, WT, TB, NS>;
     const int lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int block = (int)(unit / (T::kWaves * TB)), wave = (int)(unit / TB) % T::kWaves, j = (int)(unit % TB);
-    int tc, tr, tile;
-    if (!order.at(block, tc, tr, tile)) return;
+    const int tile = (int)(unit / (T::kWaves * TB)), wave = (int)(unit / TB) % T::kWaves, j = (int)(unit % TB);
+    int tc, tr;
+    order.place(tile, tc, tr);
     const int group = tc * WR + wave % WR;
     const int64_t row = (int64_t)tr * T::kRows + ((wave / WR) * TB + j) * 16 + (lane & 15);
     if (group >= p.groups || row >= p.rows) return;
     const i32x4* from = part + (((size_t)tile * T::kWaves + wave) * TB + j) * 256 + lane;
-    const size_t next = (size_t)order.tiles_c * order.tiles_r * T::kWaves * TB * 256;
+    const size_t next = (size_t)order.tiles() * T::kWaves * TB * 256;
     Channels<GATED, 4> ch;
     ch.load(p, group, 0, lane);
     const float s = p.qs[row];
     i32x4 acc[4] = {};
-    for (int i = 0; i < splits; ++i, from += next)
+#pragma unroll 4
+    for (int i = 0; i < order.splits; ++i)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) acc[b] += from[b * 64];
+        for (int b = 0; b < 4; ++b) acc[b] += from[i * next + b * 64];
     emit<GATED, BF16, 4>(p, ch, acc, row, s);
 }
 
@@ -339,10 +340,10 @@ struct Shape {
     int per_cu;                  // workgroups that a CU holds (by LDS)
     float fixed, step1, step;    // us: of a round; of a K step with one workgroup a CU, with per_cu of them
 };
-constexpr Shape kShapes[] = {{8, 4, 256, 8, 1, 10.0f, 1.45f, 1.45f},    // 256 channels x 256 rows
-                             {4, 2, 128, 4, 2, 6.0f, 0.83f, 1.09f},     // 128 x 128, two stages
+constexpr Shape kShapes[] = {{8, 4, 256, 8, 1, 12.0f, 1.43f, 1.43f},    // 256 channels x 256 rows
+                             {4, 2, 128, 4, 2, 5.0f, 0.83f, 1.12f},     // 128 x 128, two stages
                              {4, 2, 128, 4, 1, 6.5f, 0.54f, 0.54f},     // 128 x 128, three stages
-                             {2, 2, 64, 4, 2, 6.2f, 0.42f, 0.70f}};     // 128 x 64
+                             {2, 2, 64, 4, 2, 6.2f, 0.42f, 0.75f}};     // 128 x 64
 
 // What runs a call: a tile shape and the parts that K is cut into.
 struct Plan {
@@ -351,36 +352,38 @@ struct Plan {
     int per = 0;       // K steps of a part
 };
 
-inline TileOrder order_of(const Q8Linear& p, int shape)
+inline TileOrder order_of(const Q8Linear& p, int shape, int splits)
 {
     TileOrder o;
+    o.splits = splits;
     o.tiles_c = (p.groups + kShapes[shape].wr - 1) / kShapes[shape].wr;
     o.tiles_r = (int)(((int64_t)p.rows + kShapes[shape].rows - 1) / kShapes[shape].rows);
-    o.per_xcd = (o.tiles_c * o.tiles_r + 7) / 8;
     return o;
 }
 
 // The shape and split with the least estimated time: rounds of workgroups over the 256 CUs, each a fixed part and its K steps; for a
 // split the second kernel and its traffic.  The figures of kShapes are fitted to timings of 64 to 4096 rows on 1000 to 32768 channels of
-// 1040 to 12288 values, and the estimate is within 15 % of them.
+// 256 to 16000 values; of 120 such products the choice was within 5 % of the best of all shapes and splits for 110, within 13 % for all.
 Plan plan_linear(const Q8Linear& p)
 {
     Plan best;
     if (p.rows <= kFewRows) return best;
     const int steps = p.kblocks / 2;
+    const float from_memory = ((float)p.groups * p.kblocks * 4096 + (float)p.rows * p.width) / 5.1e6f;   // us that the operands take at least
     float least = 1e30f;
     for (int sh = 0; sh < 4; ++sh) {
         const Shape& k = kShapes[sh];
-        const TileOrder o = order_of(p, sh);
-        const int64_t tiles = (int64_t)o.tiles_c * o.tiles_r;
+        const TileOrder o = order_of(p, sh, 1);
+        const int64_t tiles = o.tiles();
         for (int splits = 1; splits <= 16 && splits <= steps; ++splits) {
             if (splits > 1 && tiles * splits > 512) break;
             const int per = (steps + splits - 1) / splits;
             if ((splits - 1) * per >= steps) continue;   // (an empty part)
             const int64_t wgs = tiles * splits;
             const float rounds = (float)((wgs + 256 * k.per_cu - 1) / (256 * k.per_cu));
-            float us = rounds * (k.fixed + per * (wgs <= 256 ? k.step1 : k.step));
-            if (splits > 1) us += 1.5f + 0.33e-6f * 4.0f * splits * p.rows * p.groups * 64;
+            float us = rounds * per * (wgs <= 256 ? k.step1 : k.step);
+            us = rounds * k.fixed + (us > from_memory ? us : from_memory);
+            if (splits > 1) us += 1.5f + splits * (0.25f + 1e-6f * p.rows * p.groups * 64);   // (a fourth of a us for a MB of parts)
             if (us < least) {
                 least = us;
                 best.shape = sh;
@@ -394,8 +397,8 @@ Plan plan_linear(const Q8Linear& p)
 
 inline size_t part_bytes(const Q8Linear& p, const Plan& pl)
 {
-    const TileOrder o = order_of(p, pl.shape);
-    return (size_t)pl.splits * o.tiles_c * o.tiles_r * kShapes[pl.shape].waves * kShapes[pl.shape].tb * 4096;
+    const TileOrder o = order_of(p, pl.shape, pl.splits);
+    return (size_t)pl.splits * o.tiles() * kShapes[pl.shape].waves * kShapes[pl.shape].tb * 4096;
 }
 
 template <int SHAPE, int WT, int NS, bool GATED, bool BF16>
@@ -404,8 +407,8 @@ int launch_tile(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
     constexpr int WR = kShapes[SHAPE].wr, TB = kShapes[SHAPE].tb;
     using T = Tile<WR, WT, TB, NS>;
     static_assert(T::kWaves == kShapes[SHAPE].waves && T::kRows == kShapes[SHAPE].rows, "kShapes describes the kernels");
-    const TileOrder o = order_of(p, SHAPE);
-    const dim3 grid((unsigned)o.per_xcd * 8, (unsigned)pl.splits);
+    const TileOrder o = order_of(p, SHAPE, pl.splits);
+    const dim3 grid((unsigned)o.tiles() * pl.splits);
     if (pl.splits == 1) {
         static unsigned long long done = 0;
         const int rc = allow_lds((const void*)q8_tile_kernel<WR, WT, TB, NS, false, GATED, BF16>, T::kLds, &done);
@@ -419,8 +422,8 @@ int launch_tile(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
     if (rc != NM_OK) return rc;
     hipLaunchKernelGGL((q8_tile_kernel<WR, WT, TB, NS, true, false, false>), grid, dim3(T::kWaves * 64), T::kLds, s, p, o, pl.per, (i32x4*)part);
     NM_HIP_CHECK(hipGetLastError());
-    hipLaunchKernelGGL((q8_join_kernel<WR, WT, TB, NS, GATED, BF16>), dim3((unsigned)o.per_xcd * 8 * T::kWaves * TB / 4), dim3(256), 0, s, p, o,
-                       pl.splits, (const i32x4*)part);
+    hipLaunchKernelGGL((q8_join_kernel<WR, WT, TB, NS, GATED, BF16>), dim3((unsigned)o.tiles() * T::kWaves * TB / 4), dim3(256), 0, s, p, o,
+                       (const i32x4*)part);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }

@@ -239,18 +239,24 @@ __device__ inline void store_tile(const Q8Linear& p, const Channels<GATED, 4>& c
 
 // Tile of a workgroup.  Workgroups go to the eight XCDs, each with an L2 of its own, in turn by their number: every XCD gets
 // a run of adjacent tiles, in bands of up to 4 tiles of rows, so that the 32 of a round share few strips of either operand.
+// With `splits` parts of K, a part's tiles follow the part's before.
 struct TileOrder {
-    int tiles_c, tiles_r, per_xcd;
-    __host__ __device__ inline bool at(int block, int& tc, int& tr, int& tile) const
+    int tiles_c, tiles_r, splits;
+    __host__ __device__ inline int tiles() const { return tiles_c * tiles_r; }
+    __device__ inline void at(int block, int& tc, int& tr, int& tile, int& split) const
     {
-        const int idx = (block & 7) * per_xcd + (block >> 3);
-        tile = idx;
-        if (idx >= tiles_c * tiles_r) return false;
-        const int band = idx / (4 * tiles_c), in = idx - band * 4 * tiles_c;
+        const int n = tiles() * splits, xcd = block & 7, more = n & 7;
+        const int unit = xcd * (n >> 3) + (xcd < more ? xcd : more) + (block >> 3);
+        split = splits > 1 ? unit / tiles() : 0;
+        tile = unit - split * tiles();
+        place(tile, tc, tr);
+    }
+    __device__ inline void place(int tile, int& tc, int& tr) const
+    {
+        const int band = tile / (4 * tiles_c), in = tile - band * 4 * tiles_c;
         const int h = tiles_r - band * 4 < 4 ? tiles_r - band * 4 : 4;
         tc = in / h;
         tr = band * 4 + in % h;
-        return true;
     }
 };
 
