@@ -104,22 +104,30 @@ __global__ __launch_bounds__(NW * 64) void q8_few_kernel(Q8Linear p)
 
 // ---------------------------------------------------------------- many rows
 // A workgroup of WR x WT wavefronts owns 64 * WR packed channels x 16 * TB * WT rows of q; a wavefront 64 x 16 TB of them.
-// K goes by in steps of 128: both operands' next step is loaded straight into LDS while the present one is multiplied.
+// K goes by in steps of 128.  LDS holds NSW steps' weights and NSQ steps' rows, loaded straight into it: while a step is multiplied, the
+// next one's lie there and later ones' are on their way.  Operands are read from LDS half a step ahead, into the other half of
+// the operand registers, so one barrier a step is enough.  Where two stages of both fill half of a CU's LDS or all of it, a third
+// of the weights still fits, and a third of the rows does not: 8192 x 4096 -> 16384 442 -> 434 us, 512 x 4096 -> 2 x 8192 41 -> 38; a third of the
+// rows instead gave 435 and 41.
 // Weights lie in LDS as in memory (a wavefront's operand is 1 KiB of adjacent bytes); a row's 128 bytes are 8 chunks of 16,
 // chunk c stored at c ^ (row & 7), so that the 8 rows that an LDS cycle reads lie in 8 different places.
 // SPLIT: a workgroup takes `per` of the K steps and stores its integer sums as they lie in the registers,
 //   part[split][tile][wave][16-row block][4 blocks][64 lanes], for q8_join_kernel to add and scale.
-template <int WR, int WT, int TB, int NS> struct Tile {
+template <int WR, int WT, int TB, int NSW, int NSQ> struct Tile {
     static constexpr int kWaves = WR * WT, kRows = 16 * TB * WT;
-    static constexpr int kWBytes = WR * 8192, kQBytes = kRows * 128, kStage = kWBytes + kQBytes, kLds = NS * kStage;
-    static constexpr int kLoads = kStage / 1024 / kWaves, kWLoads = kWBytes / 1024 / kWaves;   // of 1 KiB, a wavefront and step
+    static constexpr int kWBytes = WR * 8192, kQBytes = kRows * 128, kQAt = NSW * kWBytes, kLds = kQAt + NSQ * kQBytes;
+    static constexpr int kWLoads = kWBytes / 1024 / kWaves, kQLoads = kQBytes / 1024 / kWaves;   // of 1 KiB, a wavefront and step
     static_assert(kWBytes % (1024 * kWaves) == 0 && kQBytes % (1024 * kWaves) == 0, "every wavefront issues the same loads");
+    // Loads that may be out while a step waits for the stages of the next: those of later steps.  The operand with fewer stages is
+    // loaded first, so the other's stage that goes with it may be out too.
+    static constexpr int kFew = NSW < NSQ ? NSW : NSQ;
+    static constexpr int kOut = (kFew - 2) * (kWLoads + kQLoads) + (NSW < NSQ ? kQLoads : NSQ < NSW ? kWLoads : 0);
 };
 
-template <int WR, int WT, int TB, int NS, bool SPLIT, bool GATED, bool BF16>
+template <int WR, int WT, int TB, int NSW, int NSQ, bool SPLIT, bool GATED, bool BF16>
 __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileOrder order, int per, i32x4* part)
 {
-    using T = Tile<WR, WT, TB, NS>;
+    using T = Tile<WR, WT, TB, NSW, NSQ>;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wr = wave % WR, wt = wave / WR;
@@ -134,28 +142,35 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
     const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + (size_t)g0 * p.kblocks * 4096, (unsigned)ngrp * p.kblocks * 4096);
     const __amdgpu_buffer_rsrc_t qsr = q8_rsrc(p.q + row0 * p.ldq, rows_extent(p, nrow));
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem;
-    unsigned voff[T::kLoads];
+    unsigned wvoff[T::kWLoads], qvoff[T::kQLoads];
 #pragma unroll
-    for (int i = 0; i < T::kLoads; ++i) {
+    for (int i = 0; i < T::kWLoads; ++i) {
         const int c = wave + i * T::kWaves;   // 1 KiB of the stage
-        if (i < T::kWLoads) {
-            voff[i] = ((unsigned)(c >> 3) * p.kblocks + first * 2) * 4096 + (c & 7) * 1024 + lane * 16;
-        } else {
-            const int row = (c - T::kWBytes / 1024) * 8 + (lane >> 3);
-            voff[i] = (unsigned)(row * p.ldq) + first * 128 + (((lane & 7) ^ (row & 7)) << 4);
-        }
+        wvoff[i] = ((unsigned)(c >> 3) * p.kblocks + first * 2) * 4096 + (c & 7) * 1024 + lane * 16;
     }
-    auto fetch = [&](int i, unsigned at, bool there) {   // load i of a stage; past the last step nothing is read, so that the count of loads holds
-        const int c = wave + i * T::kWaves;
-        const bool weights = i < T::kWLoads;
-        load_to_lds(weights ? wsr : qsr, there ? voff[i] : kPast, lds0 + at + c * 1024);
-        voff[i] += weights ? 8192 : 128;
+#pragma unroll
+    for (int i = 0; i < T::kQLoads; ++i) {
+        const int row = (wave + i * T::kWaves) * 8 + (lane >> 3);
+        qvoff[i] = (unsigned)(row * p.ldq) + first * 128 + (((lane & 7) ^ (row & 7)) << 4);
+    }
+    // load i of a step's stages, weights at `wat`, rows at `qat`; past the last step nothing is read, so that the count of loads holds
+    constexpr bool WFIRST = NSW <= NSQ;
+    auto fetch = [&](int i, unsigned wat, bool wthere, unsigned qat, bool qthere) {
+        if (WFIRST ? i < T::kWLoads : i >= T::kQLoads) {
+            const int n = WFIRST ? i : i - T::kQLoads;
+            load_to_lds(wsr, wthere ? wvoff[n] : kPast, lds0 + wat + (wave + n * T::kWaves) * 1024);
+            wvoff[n] += 8192;
+        } else {
+            const int n = WFIRST ? i - T::kWLoads : i;
+            load_to_lds(qsr, qthere ? qvoff[n] : kPast, lds0 + T::kQAt + qat + (wave + n * T::kWaves) * 1024);
+            qvoff[n] += 128;
+        }
     };
     const int wlane = wr * 8192 + lane * 16;
-    const int qlane = T::kWBytes + (wt * TB * 16 + (lane & 15)) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
+    const int qlane = T::kQAt + (wt * TB * 16 + (lane & 15)) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
     i32x4 f[2][4 + TB];   // operands of the two halves of a step: 4 blocks of weights, TB of rows
-    auto read = [&](int h, int i, unsigned at) {
-        f[h][i] = *reinterpret_cast<const i32x4*>(smem + at + (i < 4 ? wlane + h * 4096 + i * 1024 : (qlane ^ (h * 64)) + (i - 4) * 2048));
+    auto read = [&](int h, int i, unsigned wat, unsigned qat) {
+        f[h][i] = *reinterpret_cast<const i32x4*>(smem + (i < 4 ? wat + wlane + h * 4096 + i * 1024 : qat + (qlane ^ (h * 64)) + (i - 4) * 2048));
     };
     constexpr bool EARLY = !SPLIT && TB < 8;   // the scales come with the first stages where the registers last for it
     Channels<GATED, 4> ch;
@@ -175,39 +190,46 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
         else return scale_of(j);
     };
     i32x4 acc[TB][4] = {};
+    constexpr int LOADS = T::kWLoads + T::kQLoads, FEW = T::kFew, MORE = NSW + NSQ - FEW;
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
+    for (int s = 0; s < FEW; ++s)
 #pragma unroll
-        for (int i = 0; i < T::kLoads; ++i) fetch(i, s * T::kStage, s < steps);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((NS - 1) * T::kLoads) : "memory");
+        for (int i = 0; i < LOADS; ++i) fetch(i, s * T::kWBytes, s < steps, s * T::kQBytes, s < steps);
 #pragma unroll
-    for (int i = 0; i < 4 + TB; ++i) read(0, i, 0);
-    unsigned now = 0;   // the stage that is multiplied
+    for (int s = FEW; s < MORE; ++s)   // the operand with more stages: the second part of a step's loads
+#pragma unroll
+        for (int i = WFIRST ? T::kWLoads : T::kQLoads; i < LOADS; ++i) fetch(i, s * T::kWBytes, s < steps, s * T::kQBytes, s < steps);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((FEW - 1) * LOADS + (MORE - FEW) * (WFIRST ? T::kQLoads : T::kWLoads)) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4 + TB; ++i) read(0, i, 0, 0);
+    unsigned wnow = 0, qnow = 0;   // the stages that are multiplied
     for (int k = 0; k < steps; ++k) {
-        const unsigned next = now + T::kStage == T::kLds ? 0 : now + T::kStage;
+        const unsigned wnext = wnow + T::kWBytes == NSW * T::kWBytes ? 0 : wnow + T::kWBytes;
+        const unsigned qnext = qnow + T::kQBytes == NSQ * T::kQBytes ? 0 : qnow + T::kQBytes;
         // first half: its operands are in registers; the second half's are read meanwhile
 #pragma unroll
         for (int j = 0; j < TB; ++j) {
 #pragma unroll
-            for (int i = j * (4 + TB) / TB; i < (j + 1) * (4 + TB) / TB; ++i) read(1, i, now);
+            for (int i = j * (4 + TB) / TB; i < (j + 1) * (4 + TB) / TB; ++i) read(1, i, wnow, qnow);
 #pragma unroll
             for (int b = 0; b < 4; ++b) acc[j][b] = mma(f[0][b], f[0][4 + j], acc[j][b]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // this stage has been read, the next one has landed
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((NS - 2) * T::kLoads) : "memory");
-        // second half: the next step's first operands are read, the stage after the last one in LDS is loaded in this one's place
+        // these stages have been read, the next ones have landed
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(T::kOut) : "memory");
+        // second half: the next step's first operands are read, and what comes after the last stages in LDS is loaded in these ones' place
 #pragma unroll
         for (int j = 0; j < TB; ++j) {
 #pragma unroll
-            for (int i = j * (4 + TB) / TB; i < (j + 1) * (4 + TB) / TB; ++i) read(0, i, next);
+            for (int i = j * (4 + TB) / TB; i < (j + 1) * (4 + TB) / TB; ++i) read(0, i, wnext, qnext);
 #pragma unroll
-            for (int i = j * T::kLoads / TB; i < (j + 1) * T::kLoads / TB; ++i) fetch(i, now, k + NS < steps);
+            for (int i = j * LOADS / TB; i < (j + 1) * LOADS / TB; ++i) fetch(i, wnow, k + NSW < steps, qnow, k + NSQ < steps);
 #pragma unroll
             for (int b = 0; b < 4; ++b) acc[j][b] = mma(f[1][b], f[1][4 + j], acc[j][b]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        now = next;
+        wnow = wnext;
+        qnow = qnext;
     }
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // no load into LDS outlives the workgroup
     if constexpr (SPLIT) {
@@ -229,10 +251,10 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
 }
 
 // Adds the sums of `splits` parts and stores the results: a wavefront takes 16 rows x 64 packed channels.
-template <int WR, int WT, int TB, int NS, bool GATED, bool BF16>
+template <int WR, int WT, int TB, int NSW, int NSQ, bool GATED, bool BF16>
 __global__ __launch_bounds__(256) void q8_join_kernel(Q8Linear p, TileOrder order, const i32x4* part)
 {
-    using T = Tile<WR, WT, TB, NS>;
+    using T = Tile<WR, WT, TB, NSW, NSQ>;
     const int lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tile = (int)(unit / (T::kWaves * TB)), wave = (int)(unit / TB) % T::kWaves, j = (int)(unit % TB);
@@ -340,9 +362,9 @@ struct Shape {
     int per_cu;                  // workgroups that a CU holds (by LDS)
     float fixed, step1, step;    // us: of a round; of a K step with one workgroup a CU, with per_cu of them
 };
-constexpr Shape kShapes[] = {{8, 4, 256, 8, 1, 12.0f, 1.43f, 1.43f},    // 256 channels x 256 rows
-                             {4, 2, 128, 4, 2, 5.0f, 0.83f, 1.12f},     // 128 x 128, two stages
-                             {4, 2, 128, 4, 1, 6.5f, 0.54f, 0.54f},     // 128 x 128, three stages
+constexpr Shape kShapes[] = {{8, 4, 256, 8, 1, 12.0f, 1.40f, 1.40f},    // 256 channels x 256 rows
+                             {4, 2, 128, 4, 2, 5.0f, 0.80f, 1.05f},     // 128 x 128, 80 KiB of LDS
+                             {4, 2, 128, 4, 1, 6.5f, 0.54f, 0.54f},     // 128 x 128, 96 KiB: three stages of rows too
                              {2, 2, 64, 4, 2, 6.2f, 0.42f, 0.75f}};     // 128 x 64
 
 // What runs a call: a tile shape and the parts that K is cut into.
@@ -401,28 +423,28 @@ inline size_t part_bytes(const Q8Linear& p, const Plan& pl)
     return (size_t)pl.splits * o.tiles() * kShapes[pl.shape].waves * kShapes[pl.shape].tb * 4096;
 }
 
-template <int SHAPE, int WT, int NS, bool GATED, bool BF16>
+template <int SHAPE, int WT, int NSW, int NSQ, bool GATED, bool BF16>
 int launch_tile(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
 {
     constexpr int WR = kShapes[SHAPE].wr, TB = kShapes[SHAPE].tb;
-    using T = Tile<WR, WT, TB, NS>;
+    using T = Tile<WR, WT, TB, NSW, NSQ>;
     static_assert(T::kWaves == kShapes[SHAPE].waves && T::kRows == kShapes[SHAPE].rows, "kShapes describes the kernels");
     const TileOrder o = order_of(p, SHAPE, pl.splits);
     const dim3 grid((unsigned)o.tiles() * pl.splits);
     if (pl.splits == 1) {
         static unsigned long long done = 0;
-        const int rc = allow_lds((const void*)q8_tile_kernel<WR, WT, TB, NS, false, GATED, BF16>, T::kLds, &done);
+        const int rc = allow_lds((const void*)q8_tile_kernel<WR, WT, TB, NSW, NSQ, false, GATED, BF16>, T::kLds, &done);
         if (rc != NM_OK) return rc;
-        hipLaunchKernelGGL((q8_tile_kernel<WR, WT, TB, NS, false, GATED, BF16>), grid, dim3(T::kWaves * 64), T::kLds, s, p, o, 0, (i32x4*)nullptr);
+        hipLaunchKernelGGL((q8_tile_kernel<WR, WT, TB, NSW, NSQ, false, GATED, BF16>), grid, dim3(T::kWaves * 64), T::kLds, s, p, o, 0, (i32x4*)nullptr);
         NM_HIP_CHECK(hipGetLastError());
         return NM_OK;
     }
     static unsigned long long done = 0;
-    const int rc = allow_lds((const void*)q8_tile_kernel<WR, WT, TB, NS, true, false, false>, T::kLds, &done);
+    const int rc = allow_lds((const void*)q8_tile_kernel<WR, WT, TB, NSW, NSQ, true, false, false>, T::kLds, &done);
     if (rc != NM_OK) return rc;
-    hipLaunchKernelGGL((q8_tile_kernel<WR, WT, TB, NS, true, false, false>), grid, dim3(T::kWaves * 64), T::kLds, s, p, o, pl.per, (i32x4*)part);
+    hipLaunchKernelGGL((q8_tile_kernel<WR, WT, TB, NSW, NSQ, true, false, false>), grid, dim3(T::kWaves * 64), T::kLds, s, p, o, pl.per, (i32x4*)part);
     NM_HIP_CHECK(hipGetLastError());
-    hipLaunchKernelGGL((q8_join_kernel<WR, WT, TB, NS, GATED, BF16>), dim3((unsigned)o.tiles() * T::kWaves * TB / 4), dim3(256), 0, s, p, o,
+    hipLaunchKernelGGL((q8_join_kernel<WR, WT, TB, NSW, NSQ, GATED, BF16>), dim3((unsigned)o.tiles() * T::kWaves * TB / 4), dim3(256), 0, s, p, o,
                        (const i32x4*)part);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
@@ -432,10 +454,10 @@ template <bool GATED, bool BF16>
 int pick_linear(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
 {
     switch (pl.shape) {
-    case 0: return launch_tile<0, 2, 2, GATED, BF16>(p, pl, part, s);
-    case 1: return launch_tile<1, 2, 2, GATED, BF16>(p, pl, part, s);
-    case 2: return launch_tile<2, 2, 3, GATED, BF16>(p, pl, part, s);
-    case 3: return launch_tile<3, 1, 3, GATED, BF16>(p, pl, part, s);
+    case 0: return launch_tile<0, 2, 3, 2, GATED, BF16>(p, pl, part, s);
+    case 1: return launch_tile<1, 2, 3, 2, GATED, BF16>(p, pl, part, s);
+    case 2: return launch_tile<2, 2, 3, 3, GATED, BF16>(p, pl, part, s);
+    case 3: return launch_tile<3, 1, 3, 3, GATED, BF16>(p, pl, part, s);
     default: break;
     }
     if (p.rows <= 16) return pick_few<1, GATED, BF16>(p, s);
