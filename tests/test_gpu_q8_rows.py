@@ -140,6 +140,23 @@ def test_no_rows_more_axes_and_many_rows():
     assert torch.equal(nm.nm_dequantize_q8(q, s), q.float() * s[:, None])
 
 
+@pytest.mark.parametrize("norm", [False, True])
+def test_workgroups_that_take_several_rows(norm):
+    """More rows than workgroups, and rows that a workgroup's wavefronts share: one row's reductions do not meet the next one's."""
+    rows, width = (1 << 20) + 5000, 1032
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((4096, width), generator=g, device="cuda").to(torch.bfloat16)
+    x *= torch.exp(torch.randn(4096, generator=g, device="cuda") * 3)[:, None].to(torch.bfloat16)
+    many = x.repeat(rows // 4096 + 1, 1)[:rows]
+    say(f"{rows} rows of {width}, norm {norm}")
+    call = (lambda t: nm.nm_rmsnorm_q8(t)[:2]) if norm else nm.nm_quantize_q8
+    q0, s0 = call(x)
+    q, s = call(many)
+    for i in range(0, rows, 4096):
+        n = min(4096, rows - i)
+        assert torch.equal(q[i:i + n], q0[:n]) and torch.equal(s[i:i + n], s0[:n])
+
+
 def test_offsets_past_32_bits():
     """Rows whose bytes lie more than 4 GiB apart."""
     rows, width, ld = 3, 1000, 1 << 24
