@@ -324,7 +324,8 @@ int nm_linear_q8_workspace(const int8_t* q, int64_t rows, int64_t ldq, const nm_
     p.gated = w->gated;
     p.groups = w->groups;
     p.kblocks = w->kblocks;
-    *bytes = rows ? q8_linear_workspace(p) : 0;
+    const Q8Plan plan = rows ? q8_plan(p) : Q8Plan{};
+    *bytes = plan.rows_bytes + plan.part_bytes;
     return NM_OK;
 }
 
@@ -386,7 +387,8 @@ int nm_linear_q8(const int8_t* q, int64_t rows, int width, int64_t ldq, const fl
     // 8192 x 4096 -> 16384 (268 MB) 422 us past the cache and 455 through it, 4096 x 4096 -> 24576 (201 MB) 323 and 340;
     // 16384 x 1024 -> 4096 (134 MB) 89 and 83
     p.past = (size_t)rows * outs * es > ((size_t)160 << 20);
-    const size_t need = q8_linear_workspace(p);
+    const Q8Plan plan = q8_plan(p);
+    const size_t need = plan.rows_bytes + plan.part_bytes;
     if (need) {
         if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16) {
             set_error("this call needs %zu bytes of workspace, 16-byte aligned; %zu were given", need,
@@ -400,7 +402,7 @@ int nm_linear_q8(const int8_t* q, int64_t rows, int width, int64_t ldq, const fl
         NM_TRY(check_apart("workspace", sw, "residual", sr, false));
         NM_TRY(check_apart("workspace", sw, "y", sy, false));
     }
-    return run_q8_linear(p, workspace, (hipStream_t)stream);
+    return run_q8_linear(p, plan, workspace, (hipStream_t)stream);
 }
 
 // The integers of a block are 64 bits wide; one that does not fit an int is out of range for every argument that is one.

@@ -63,7 +63,15 @@ struct Q8Linear {
     int gated, groups, kblocks, y_bf16;
     int past;   // y is stored past the last-level cache
 };
-size_t q8_linear_workspace(const Q8Linear& p);
-int run_q8_linear(const Q8Linear& p, void* workspace, hipStream_t s);
+// What runs a call: a tile shape and the parts that K is cut into; and the workspace: rows of q at a stride that the kernels can read,
+// if theirs is none, then the parts of a divided sum.
+struct Q8Plan {
+    int shape = -1;    // -1: the few-row kernels
+    int splits = 1;
+    int per = 0;       // K steps of a part
+    size_t rows_bytes = 0, part_bytes = 0;
+};
+Q8Plan q8_plan(const Q8Linear& p);
+int run_q8_linear(const Q8Linear& p, const Q8Plan& plan, void* workspace, hipStream_t s);
 
 }  // namespace nm

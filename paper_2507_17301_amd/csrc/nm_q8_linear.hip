@@ -5,7 +5,7 @@
 // The sum is in 32-bit integers and exact, so no split of K changes a result.  Weights are the first operand of the
 // 16x16x64 integer matrix instruction, rows of q the second: lane l of a wavefront then holds packed weight rows
 // 4 (l / 16) .. + 3 of a 16-row block for row l % 16 of q, and the packing deals channels so that the four blocks of
-// a 64-row group give it 16 adjacent channels (gated: 8 adjacent outputs, gate and value in the same registers).
+// a 64-row group give it twice 8 adjacent channels (gated: 8 adjacent outputs, gate and value in the same registers).
 #include "nm_q8_product.h"
 
 namespace nm {
@@ -17,7 +17,7 @@ namespace {
 // once, there is nothing to share.  Rows of q go through LDS, a part of it for each wavefront, so that 8 lanes read the 128
 // adjacent bytes of a row: read straight into operand registers, 16 rows with 64 bytes each an instruction, they come at a third
 // of the rate (38 instead of 120 bytes a ns and CU out of the L2), and 64 rows x 4096 x 4096 took 11.4 us instead of 8.7.
-// Bound by the weights' bytes: see pick_few for the times.
+// Bound by the weights' bytes: 16 rows x 4096 -> 24576 in 18.6 us, 5.4 TB/s of them (pick_few has more).
 template <int TB, int RB, int NW, int U> constexpr int few_lds()
 {
     const int rows = NW * U * TB * 2048, sums = NW * RB * TB * 1024;
@@ -106,9 +106,12 @@ __global__ __launch_bounds__(NW * 64) void q8_few_kernel(Q8Linear p)
 // A workgroup of WR x WT wavefronts owns 64 * WR packed channels x 16 * TB * WT rows of q; a wavefront 64 x 16 TB of them.
 // K goes by in steps of 128.  LDS holds NSW steps' weights and NSQ steps' rows, loaded straight into it: while a step is multiplied, the
 // next one's lie there and later ones' are on their way.  Operands are read from LDS half a step ahead, into the other half of
-// the operand registers, so one barrier a step is enough.  Where two stages of both fill half of a CU's LDS or all of it, a third
-// of the weights still fits, and a third of the rows does not: 8192 x 4096 -> 16384 442 -> 434 us, 512 x 4096 -> 2 x 8192 41 -> 38; a third of the
-// rows instead gave 435 and 41.
+// the operand registers, so one barrier a step is enough.  Beside two stages of each, a third of one operand still fits a CU's LDS
+// (half of it, for two workgroups); of the weights it gave most: 8192 x 4096 -> 16384 442 -> 434 us, 512 x 4096 -> 2 x 8192 41 -> 38, of the rows
+// 436 and 41.
+// Bound by the power limit on large products: 8192 x 4096 -> 16384 takes 430 us, 2.56 POP/s, at 1.86 GHz with the matrix units busy 64 % of
+// the cycles; the 256 x 256 loop without any load or barrier takes 1.16 us a step on such values (0.91 on zeros, 0.85 at 2.4 GHz by the
+// instruction's 16 cycles), with them 1.38 (0.98).
 // Weights lie in LDS as in memory (a wavefront's operand is 1 KiB of adjacent bytes); a row's 128 bytes are 8 chunks of 16,
 // chunk c stored at c ^ (row & 7), so that the 8 rows that an LDS cycle reads lie in 8 different places.
 // SPLIT: a workgroup takes `per` of the K steps and stores its integer sums as they lie in the registers,
@@ -250,7 +253,9 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
     }
 }
 
-// Adds the sums of `splits` parts and stores the results: a wavefront takes 16 rows x 64 packed channels.
+// Adds the sums of a tile's parts and stores the results: a wavefront takes 16 rows x 64 packed channels, so that few tiles still
+// make many wavefronts.  Bound by the parts' bytes, which the last-level cache holds: 128 x 12288 -> 4096 in 8 parts takes 22 us with
+// it, 58 as 32 undivided tiles.
 template <int WR, int WT, int TB, int NSW, int NSQ, bool GATED, bool BF16>
 __global__ __launch_bounds__(256) void q8_join_kernel(Q8Linear p, TileOrder order, const i32x4* part)
 {
@@ -276,7 +281,8 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8Linear p, TileOrder orde
     emit<GATED, BF16, 4>(p, ch, acc, row, s);
 }
 
-// Rows copied to ones at a stride of `pitch` bytes, a multiple of 16 (the bytes past a row's end are zero).
+// Rows copied to ones at a stride of `pitch` bytes, a multiple of 16 (the bytes past a row's end are zero).  333 x 1037: 2.7 us, the
+// time of a small launch.
 __global__ __launch_bounds__(256) void q8_align_kernel(const int8_t* q, int64_t ldq, int8_t* to, int pitch, int rows, int width)
 {
     const int c = (blockIdx.x * 256 + threadIdx.x) * 16;
@@ -367,13 +373,6 @@ constexpr Shape kShapes[] = {{8, 4, 256, 8, 1, 12.0f, 1.40f, 1.40f},    // 256 c
                              {4, 2, 128, 4, 1, 6.5f, 0.54f, 0.54f},     // 128 x 128, 96 KiB: three stages of rows too
                              {2, 2, 64, 4, 2, 6.2f, 0.42f, 0.75f}};     // 128 x 64
 
-// What runs a call: a tile shape and the parts that K is cut into.
-struct Plan {
-    int shape = -1;    // -1: the few-row kernels
-    int splits = 1;
-    int per = 0;       // K steps of a part
-};
-
 inline TileOrder order_of(const Q8Linear& p, int shape, int splits)
 {
     TileOrder o;
@@ -386,9 +385,9 @@ inline TileOrder order_of(const Q8Linear& p, int shape, int splits)
 // The shape and split with the least estimated time: rounds of workgroups over the 256 CUs, each a fixed part and its K steps; for a
 // split the second kernel and its traffic.  The figures of kShapes are fitted to timings of 64 to 4096 rows on 1000 to 32768 channels of
 // 256 to 16000 values; of 120 such products the choice was within 5 % of the best of all shapes and splits for 110, within 13 % for all.
-Plan plan_linear(const Q8Linear& p)
+Q8Plan plan_linear(const Q8Linear& p)
 {
-    Plan best;
+    Q8Plan best;
     if (p.rows <= kFewRows) return best;
     const int steps = p.kblocks / 2;
     const float from_memory = ((float)p.groups * p.kblocks * 4096 + (float)p.rows * p.width) / 5.1e6f;   // us that the operands take at least
@@ -417,14 +416,14 @@ Plan plan_linear(const Q8Linear& p)
     return best;
 }
 
-inline size_t part_bytes(const Q8Linear& p, const Plan& pl)
+inline size_t part_bytes(const Q8Linear& p, const Q8Plan& pl)
 {
     const TileOrder o = order_of(p, pl.shape, pl.splits);
     return (size_t)pl.splits * o.tiles() * kShapes[pl.shape].waves * kShapes[pl.shape].tb * 4096;
 }
 
 template <int SHAPE, int WT, int NSW, int NSQ, bool GATED, bool BF16>
-int launch_tile(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
+int launch_tile(const Q8Linear& p, const Q8Plan& pl, void* part, hipStream_t s)
 {
     constexpr int WR = kShapes[SHAPE].wr, TB = kShapes[SHAPE].tb;
     using T = Tile<WR, WT, TB, NSW, NSQ>;
@@ -451,7 +450,7 @@ int launch_tile(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
 }
 
 template <bool GATED, bool BF16>
-int pick_linear(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
+int pick_linear(const Q8Linear& p, const Q8Plan& pl, void* part, hipStream_t s)
 {
     switch (pl.shape) {
     case 0: return launch_tile<0, 2, 3, 2, GATED, BF16>(p, pl, part, s);
@@ -465,44 +464,30 @@ int pick_linear(const Q8Linear& p, const Plan& pl, void* part, hipStream_t s)
     return pick_few<4, GATED, BF16>(p, s);
 }
 
-// The workspace: rows of q at a stride that the kernels can read, if theirs is none, then the parts of a split sum.
-struct Layout {
-    Plan plan;
-    size_t rows_bytes = 0, part_bytes = 0;
-    int pitch = 0;
-};
-Layout layout_of(const Q8Linear& p)
-{
-    Layout l;
-    l.plan = plan_linear(p);
-    l.pitch = (p.width + 15) / 16 * 16;
-    if (!aligned16(p)) l.rows_bytes = (size_t)p.rows * l.pitch;
-    if (l.plan.splits > 1) l.part_bytes = part_bytes(p, l.plan);
-    return l;
-}
-
 }  // namespace
 
-size_t q8_linear_workspace(const Q8Linear& p)
+Q8Plan q8_plan(const Q8Linear& p)
 {
-    const Layout l = layout_of(p);
-    return l.rows_bytes + l.part_bytes;
+    Q8Plan pl = plan_linear(p);
+    if (!aligned16(p)) pl.rows_bytes = (size_t)p.rows * ((p.width + 15) / 16 * 16);
+    if (pl.splits > 1) pl.part_bytes = part_bytes(p, pl);
+    return pl;
 }
 
-int run_q8_linear(const Q8Linear& call, void* workspace, hipStream_t s)
+int run_q8_linear(const Q8Linear& call, const Q8Plan& pl, void* workspace, hipStream_t s)
 {
     Q8Linear p = call;
-    const Layout l = layout_of(p);
-    if (l.rows_bytes) {
-        const dim3 grid((unsigned)(l.pitch / 16 + 255) / 256, (unsigned)(p.rows < 4096 ? p.rows : 4096));
-        hipLaunchKernelGGL(q8_align_kernel, grid, dim3(256), 0, s, p.q, p.ldq, (int8_t*)workspace, l.pitch, p.rows, p.width);
+    if (pl.rows_bytes) {
+        const int pitch = (p.width + 15) / 16 * 16;
+        const dim3 grid((unsigned)(pitch / 16 + 255) / 256, (unsigned)(p.rows < 4096 ? p.rows : 4096));
+        hipLaunchKernelGGL(q8_align_kernel, grid, dim3(256), 0, s, p.q, p.ldq, (int8_t*)workspace, pitch, p.rows, p.width);
         NM_HIP_CHECK(hipGetLastError());
         p.q = (const int8_t*)workspace;
-        p.ldq = l.pitch;
+        p.ldq = pitch;
     }
-    void* part = (char*)workspace + l.rows_bytes;
-    if (p.gated) return p.y_bf16 ? pick_linear<true, true>(p, l.plan, part, s) : pick_linear<true, false>(p, l.plan, part, s);
-    return p.y_bf16 ? pick_linear<false, true>(p, l.plan, part, s) : pick_linear<false, false>(p, l.plan, part, s);
+    void* part = (char*)workspace + pl.rows_bytes;
+    if (p.gated) return p.y_bf16 ? pick_linear<true, true>(p, pl, part, s) : pick_linear<true, false>(p, pl, part, s);
+    return p.y_bf16 ? pick_linear<false, true>(p, pl, part, s) : pick_linear<false, false>(p, pl, part, s);
 }
 
 int run_q8_pack(const int8_t* w, int64_t ldw, const float* scales, const nm_q8* h, int* d_bad, hipStream_t s)

@@ -121,8 +121,14 @@ int run_q8_unpack(const nm_q8* h, int8_t* w, float* scales, hipStream_t)
     }
     return NM_OK;
 }
-size_t q8_linear_workspace(const Q8Linear&) { return g_workspace; }
-int run_q8_linear(const Q8Linear& p, void* ws, hipStream_t)
+Q8Plan q8_plan(const Q8Linear&)
+{
+    Q8Plan p;
+    p.rows_bytes = g_workspace / 2;
+    p.part_bytes = g_workspace - p.rows_bytes;
+    return p;
+}
+int run_q8_linear(const Q8Linear& p, const Q8Plan&, void* ws, hipStream_t)
 {
     ++g_launches;
     g_linear = p;
