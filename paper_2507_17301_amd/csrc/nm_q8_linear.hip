@@ -17,7 +17,7 @@ namespace {
 // once, there is nothing to share.  Rows of q go through LDS, a part of it for each wavefront, so that 8 lanes read the 128
 // adjacent bytes of a row: read straight into operand registers, 16 rows with 64 bytes each an instruction, they come at a third
 // of the rate (38 instead of 120 bytes a ns and CU out of the L2), and 64 rows x 4096 x 4096 took 11.4 us instead of 8.7.
-// Bound by the weights' bytes: 16 rows x 4096 -> 24576 in 18.6 us, 5.4 TB/s of them (pick_few has more).
+// Bound by the weights' bytes: 16 rows x 4096 -> 24576 in 19 us, 5.3 TB/s of them (pick_few has more).
 template <int TB, int RB, int NW, int U> constexpr int few_lds()
 {
     const int rows = NW * U * TB * 2048, sums = NW * RB * TB * 1024;
@@ -106,12 +106,12 @@ __global__ __launch_bounds__(NW * 64) void q8_few_kernel(Q8Linear p)
 // A workgroup of WR x WT wavefronts owns 64 * WR packed channels x 16 * TB * WT rows of q; a wavefront 64 x 16 TB of them.
 // K goes by in steps of 128.  LDS holds NSW steps' weights and NSQ steps' rows, loaded straight into it: while a step is multiplied, the
 // next one's lie there and later ones' are on their way.  Operands are read from LDS half a step ahead, into the other half of
-// the operand registers, so one barrier a step is enough.  Beside two stages of each, a third of one operand still fits a CU's LDS
-// (half of it, for two workgroups); of the weights it gave most: 8192 x 4096 -> 16384 442 -> 434 us, 512 x 4096 -> 2 x 8192 41 -> 38, of the rows
-// 436 and 41.
-// Bound by the power limit on large products: 8192 x 4096 -> 16384 takes 430 us, 2.56 POP/s, at 1.86 GHz with the matrix units busy 64 % of
-// the cycles; the 256 x 256 loop without any load or barrier takes 1.16 us a step on such values (0.91 on zeros, 0.85 at 2.4 GHz by the
-// instruction's 16 cycles), with them 1.38 (0.98).
+// the operand registers, so one barrier a step is enough.  Beside two stages of each, a third of one operand still fits a
+// CU's LDS (half of it, for two workgroups); of the weights it gave most: 8192 x 4096 -> 16384 442 -> 435 us,
+// 512 x 4096 -> 2 x 8192 41 -> 38, of the rows 437 and 41.
+// Bound by the power limit on large products: 8192 x 4096 -> 16384 takes 430 us, 2.56 POP/s, at 1.86 GHz with the matrix
+// units busy 64 % of the cycles; the 256 x 256 loop without any load or barrier takes 1.16 us a step on such values (0.91 on
+// zeros, 0.85 at 2.4 GHz by the instruction's 16 cycles), with them 1.38 (0.98).
 // Weights lie in LDS as in memory (a wavefront's operand is 1 KiB of adjacent bytes); a row's 128 bytes are 8 chunks of 16,
 // chunk c stored at c ^ (row & 7), so that the 8 rows that an LDS cycle reads lie in 8 different places.
 // SPLIT: a workgroup takes `per` of the K steps and stores its integer sums as they lie in the registers,
@@ -254,8 +254,8 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
 }
 
 // Adds the sums of a tile's parts and stores the results: a wavefront takes 16 rows x 64 packed channels, so that few tiles still
-// make many wavefronts.  Bound by the parts' bytes, which the last-level cache holds: 128 x 12288 -> 4096 in 8 parts takes 22 us with
-// it, 58 as 32 undivided tiles.
+// make many wavefronts.  Bound by the parts' bytes, which the last-level cache holds: 128 x 12288 -> 4096 in 4 to 8 parts takes
+// 21 to 23 us with it, 58 undivided.
 template <int WR, int WT, int TB, int NSW, int NSQ, bool GATED, bool BF16>
 __global__ __launch_bounds__(256) void q8_join_kernel(Q8Linear p, TileOrder order, const i32x4* part)
 {

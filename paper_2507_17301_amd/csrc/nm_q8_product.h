@@ -149,8 +149,8 @@ __device__ inline void emit(const Q8Linear& p, const Channels<GATED, NB>& ch, co
 
 // A workgroup's outputs through LDS, so that whole rows of its tile are stored, 16 bytes a thread and adjacent threads adjacent:
 // straight from the registers (above) a store instruction reaches 16 rows with 64 bytes each, and 8192 x 4096 -> 16384 took 433 us
-// instead of 422, 8000 x 2000 -> 5000 (rows that begin in the middle of a line) 99 instead of 92.  JP of the TB blocks of rows at a time, STAGE32 in fp32 (for a residual, so that it rounds once).
-// The 16-byte pieces of a row lie at piece ^ (row & 7).
+// instead of 422, 8000 x 2000 -> 5000 (rows that begin in the middle of a line) 99 instead of 92.  JP of the TB blocks of rows
+// at a time, STAGE32 in fp32 (for a residual, so that it rounds once).  The 16-byte pieces of a row lie at piece ^ (row & 7).
 template <int WR, int WT, int TB, int JP, bool STAGE32, bool GATED, bool BF16, typename Scale>
 __device__ inline void store_tile(const Q8Linear& p, const Channels<GATED, 4>& ch, Scale scale, const i32x4 (&acc)[TB][4], char* smem,
                                   int wr, int wt, int lane, int group0, int64_t row0)
