@@ -106,9 +106,8 @@ __global__ __launch_bounds__(NW * 64) void q8_few_kernel(Q8Linear p)
 // A workgroup of WR x WT wavefronts owns 64 * WR packed channels x 16 * TB * WT rows of q; a wavefront 64 x 16 TB of them.
 // K goes by in steps of 128.  LDS holds NSW steps' weights and NSQ steps' rows, loaded straight into it: while a step is multiplied, the
 // next one's lie there and later ones' are on their way.  Operands are read from LDS half a step ahead, into the other half of
-// the operand registers, so one barrier a step is enough.  Beside two stages of each, a third of one operand still fits a
-// CU's LDS (half of it, for two workgroups); of the weights it gave most: 8192 x 4096 -> 16384 442 -> 435 us,
-// 512 x 4096 -> 2 x 8192 41 -> 38, of the rows 437 and 41.
+// the operand registers, so one barrier a step is enough.  Three stages of each where they fit a CU's LDS; where they do not, two of
+// the rows and three of the weights (8192 x 4096 -> 16384 442 us with two of each, 435 with a third of the weights, 437 of the rows).
 // Bound by the power limit on large products: 8192 x 4096 -> 16384 takes 430 us, 2.56 POP/s, at 1.86 GHz with the matrix
 // units busy 64 % of the cycles; the 256 x 256 loop without any load or barrier takes 1.16 us a step on such values (0.91 on
 // zeros, 0.85 at 2.4 GHz by the instruction's 16 cycles), with them 1.38 (0.98).
@@ -126,6 +125,8 @@ template <int WR, int WT, int TB, int NSW, int NSQ> struct Tile {
     static constexpr int kFew = NSW < NSQ ? NSW : NSQ;
     static constexpr int kOut = (kFew - 2) * (kWLoads + kQLoads) + (NSW < NSQ ? kQLoads : NSQ < NSW ? kWLoads : 0);
 };
+
+constexpr int largest_divisor(int n, int most) { return most >= n ? n : n % most == 0 ? most : largest_divisor(n, most - 1); }
 
 template <int WR, int WT, int TB, int NSW, int NSQ, bool SPLIT, bool GATED, bool BF16>
 __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileOrder order, int per, i32x4* part)
@@ -246,8 +247,8 @@ __global__ __launch_bounds__(WR * WT * 64) void q8_tile_kernel(Q8Linear p, TileO
     } else {
         if constexpr (!EARLY) ch.load(p, group, 0, lane);
         constexpr int kFit = T::kLds / (16 * WT * 64 * WR * 4 / (GATED ? 2 : 1));   // blocks of rows that fit LDS in fp32
-        constexpr int JP4 = kFit >= TB ? TB : kFit >= TB / 2 ? TB / 2 : TB / 4, JP2 = 2 * kFit >= TB ? TB : TB / 2;
-        static_assert(JP4 <= kFit && JP2 <= 2 * kFit, "the tile's outputs go through LDS");
+        constexpr int JP4 = largest_divisor(TB, kFit), JP2 = largest_divisor(TB, 2 * kFit);
+        static_assert(kFit >= 1, "the tile's outputs go through LDS");
         if (!BF16 || p.res) store_tile<WR, WT, TB, JP4, true, GATED, BF16>(p, ch, scale, acc, smem, wr, wt, lane, g0, row0);
         else store_tile<WR, WT, TB, JP2, false, GATED, BF16>(p, ch, scale, acc, smem, wr, wt, lane, g0, row0);
     }
@@ -362,17 +363,22 @@ int pick_few(const Q8Linear& p, hipStream_t s)
     return launch_few<TB, 1, 8, U, GATED, BF16>(p, s);
 }
 
-// The tile kernels' shapes.
+// The tile kernels' shapes.  More rows or channels a workgroup take less from the L2 for a product; few of either leave CUs without
+// work or tiles half empty: over 400 products the best of these seven was 8 % faster than the best of 256 x 256, 128 x 128 and
+// 128 x 64 (300 x 4096 -> 2 x 8192 35 -> 28 us, 700 x 4096 -> 2 x 12288 97 -> 76, 2048 x 12288 -> 4096 96 -> 85); leaving any one out
+// costs 0.5 to 2 %, and 256 x 64, 128 x 256, 128 x 96 and 128 x 128 twice a CU would add 0.3 % together.
 struct Shape {
     int waves, wr, rows, tb;
     int per_cu;                  // workgroups that a CU holds (by LDS)
-    float fixed, step1, step;    // us: of a round; of a K step with one workgroup a CU, with per_cu of them
+    float fixed, step, more;     // us: of a round; of a K step; what that takes more where all CUs are full, by the share that is
 };
-constexpr Shape kShapes[] = {{8, 4, 256, 8, 1, 12.0f, 1.40f, 1.40f},    // 256 channels x 256 rows
-                             {4, 2, 128, 4, 2, 5.0f, 0.80f, 1.05f},     // 128 x 128, 80 KiB of LDS
-                             {4, 2, 128, 4, 1, 6.5f, 0.54f, 0.54f},     // 128 x 128, 96 KiB: three stages of rows too
-                             {2, 2, 64, 4, 2, 6.2f, 0.42f, 0.75f}};     // 128 x 64
-
+constexpr Shape kShapes[] = {{8, 4, 256, 8, 1, 10.4f, 0.87f, 0.54f},    // 256 channels x 256 rows
+                             {8, 4, 192, 6, 1, 7.9f, 0.71f, 0.36f},
+                             {8, 4, 128, 4, 1, 7.2f, 0.58f, 0.20f},
+                             {4, 2, 192, 6, 1, 5.6f, 0.48f, 0.21f},     // 128 channels
+                             {4, 2, 160, 5, 1, 5.6f, 0.38f, 0.20f},
+                             {4, 2, 128, 4, 1, 5.7f, 0.32f, 0.20f},
+                             {2, 2, 64, 4, 2, 6.0f, 0.18f, 0.46f}};
 inline TileOrder order_of(const Q8Linear& p, int shape, int splits)
 {
     TileOrder o;
@@ -383,28 +389,28 @@ inline TileOrder order_of(const Q8Linear& p, int shape, int splits)
 }
 
 // The shape and split with the least estimated time: rounds of workgroups over the 256 CUs, each a fixed part and its K steps; for a
-// split the second kernel and its traffic.  The figures of kShapes are fitted to timings of 64 to 4096 rows on 1000 to 32768 channels of
-// 256 to 16000 values; of 120 such products the choice was within 5 % of the best of all shapes and splits for 110, within 13 % for all.
+// split the second kernel and its traffic.  The figures are fitted to timings of 65 to 8192 rows on 300 to 24576 channels of 512 to
+// 16000 values; of 400 such products the choice was within 5 % of the best of all shapes and splits for 365, within 19 % for all.
 Q8Plan plan_linear(const Q8Linear& p)
 {
     Q8Plan best;
     if (p.rows <= kFewRows) return best;
     const int steps = p.kblocks / 2;
-    const float from_memory = ((float)p.groups * p.kblocks * 4096 + (float)p.rows * p.width) / 5.1e6f;   // us that the operands take at least
+    const float from_memory = ((float)p.groups * p.kblocks * 4096 + (float)p.rows * p.width) / 7.8e6f;   // us that the operands take at least
     float least = 1e30f;
-    for (int sh = 0; sh < 4; ++sh) {
+    for (int sh = 0; sh < (int)(sizeof(kShapes) / sizeof(Shape)); ++sh) {
         const Shape& k = kShapes[sh];
         const TileOrder o = order_of(p, sh, 1);
-        const int64_t tiles = o.tiles();
-        for (int splits = 1; splits <= 16 && splits <= steps; ++splits) {
-            if (splits > 1 && tiles * splits > 512) break;
+        const int64_t tiles = (int64_t)o.tiles_c * o.tiles_r, room = 256 * k.per_cu;
+        for (int splits = 1; splits <= 16; ++splits) {
             const int per = (steps + splits - 1) / splits;
+            if (splits > 1 && (tiles * splits > 512 || per < 3)) break;
             if ((splits - 1) * per >= steps) continue;   // (an empty part)
-            const int64_t wgs = tiles * splits;
-            const float rounds = (float)((wgs + 256 * k.per_cu - 1) / (256 * k.per_cu));
-            float us = rounds * per * (wgs <= 256 ? k.step1 : k.step);
-            us = rounds * k.fixed + (us > from_memory ? us : from_memory);
-            if (splits > 1) us += 1.5f + splits * (0.25f + 1e-6f * p.rows * p.groups * 64);   // (a fourth of a us for a MB of parts)
+            const int64_t rounds = tiles * splits / room, rest = tiles * splits % room;
+            float us = rounds * per * (k.step + k.more);
+            if (rest) us += per * (k.step + k.more * rest / room);
+            us = (rounds + (rest > 0)) * k.fixed + (us > from_memory ? us : from_memory);
+            if (splits > 1) us += 2.5f + splits * (0.09f + 0.8e-6f * p.rows * p.groups * 64);   // (a fifth of a us for a MB of parts)
             if (us < least) {
                 least = us;
                 best.shape = sh;
@@ -456,7 +462,10 @@ int pick_linear(const Q8Linear& p, const Q8Plan& pl, void* part, hipStream_t s)
     case 0: return launch_tile<0, 2, 3, 2, GATED, BF16>(p, pl, part, s);
     case 1: return launch_tile<1, 2, 3, 2, GATED, BF16>(p, pl, part, s);
     case 2: return launch_tile<2, 2, 3, 3, GATED, BF16>(p, pl, part, s);
-    case 3: return launch_tile<3, 1, 3, 3, GATED, BF16>(p, pl, part, s);
+    case 3: return launch_tile<3, 2, 3, 3, GATED, BF16>(p, pl, part, s);
+    case 4: return launch_tile<4, 2, 3, 3, GATED, BF16>(p, pl, part, s);
+    case 5: return launch_tile<5, 2, 3, 3, GATED, BF16>(p, pl, part, s);
+    case 6: return launch_tile<6, 1, 3, 3, GATED, BF16>(p, pl, part, s);
     default: break;
     }
     if (p.rows <= 16) return pick_few<1, GATED, BF16>(p, s);

@@ -78,6 +78,16 @@ def test_gated_tiles_and_divided_sums(rows, k, n, dtype):
     _product(rows, k, n, dtype, True, True, seed=rows)
 
 
+# 256 channels x 256, 192, 128 rows, 128 channels x 192, 160, 128, 64; each whole and divided
+@pytest.mark.parametrize("form", ["plain", "residual", "gated"])
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("rows,k,n", [(2696, 68, 4618), (12517, 14626, 148), (4741, 66, 1734), (8213, 12060, 134), (3273, 67, 1794),
+                                      (850, 7280, 2796), (979, 64, 5286), (165, 5056, 4684), (150, 1005, 10058), (131, 3427, 1618),
+                                      (83, 215, 68), (84, 3864, 1172), (91, 260, 78), (67, 2615, 96)])
+def test_each_shape_of_tile(rows, k, n, dtype, form):
+    _product(rows, k, n, dtype, form == "gated", True, form == "residual", seed=k)
+
+
 @pytest.mark.parametrize("rows,n,dtype,gated,residual", [(5000, 17000, "bf16", False, False), (5000, 17001, "bf16", False, True),
                                                          (3000, 14003, "f32", False, False), (6000, 30002, "bf16", True, False)])
 def test_outputs_stored_past_the_cache(rows, n, dtype, gated, residual):
