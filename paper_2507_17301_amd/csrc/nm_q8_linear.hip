@@ -6,6 +6,8 @@
 // 16x16x64 integer matrix instruction, rows of q the second: lane l of a wavefront then holds packed weight rows
 // 4 (l / 16) .. + 3 of a 16-row block for row l % 16 of q, and the packing deals channels so that the four blocks of
 // a 64-row group give it twice 8 adjacent channels (gated: 8 adjacent outputs, gate and value in the same registers).
+// (The 32x32x32 form is as fast on zeros, 4.9 POP/s out of registers, but takes more power: 3.4 POP/s on normally distributed
+// values, this one 4.0.)
 #include "nm_q8_product.h"
 
 namespace nm {
