@@ -39,7 +39,8 @@ enum { NM_Q8_MAX_WIDTH = 65536 };
 
 /*
  * nm_quantize_q8 -- every row rounded to 8 bits under its own scale:
- *   a = max |x_i|,  s = a / 127,  q_i = x_i * (127 / a) rounded to the nearest, ties to even
+ *   a = max |x_i|,  s = a / 127,  q_i = x_i * 127 / a rounded to the nearest, ties to even
+ *   Of bf16 values that is exact.  Of fp32 values, a quotient within 2.4e-5 of half way between two whole numbers may go to either.
  *   x_dev      rows of x_dtype (NM_F32 or NM_BF16) at stride ldx, only read
  *   q_dev      int8 rows at stride ldq >= width, fully overwritten (gaps between rows are not touched)
  *   scales_dev fp32 [rows]

@@ -1,6 +1,6 @@
 // Row operators in 8 bits: residual addition + root-mean-square norm + rounding, rounding alone, reading back.
 //
-//   h = x + r;  v = gamma * h / sqrt(mean(h^2) + eps);  s = max|v| / 127;  q = rint(v * 127 / max|v|)
+//   h = x + r;  v = gamma * h / sqrt(mean(h^2) + eps);  s = max|v| / 127;  q = rint(v * 127 / max|v|), ties to even
 //
 // Bound by HBM: a value is read once (twice with a residual), kept in registers over both reductions (sum of
 // squares, largest magnitude), and written once.  NT threads share a row, 8 adjacent values a thread at a time,
@@ -154,8 +154,10 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
         if (t == 0) p.scales[row] = bad ? __uint_as_float(0x7fc00000u) : none ? 0.0f : a / 127.0f;
         int8_t* pq = p.q + row * p.ldq;
         const bool zero = bad || none;
-        // 1.5 * 2^23 + n holds n, rounded to nearest even by the addition, in its low bits
-        auto round8 = [&](float f) { return zero ? 0u : __float_as_uint(fmaf(f, inv, 12582912.0f)) & 0xffu; };
+        // 1.5 * 2^23 + n holds n, rounded to nearest even by the addition, in its low bits.  Before that a product is rounded to a multiple of
+        // 2^-15, the spacing of fp32 next to 384: the error of 127 / a moves it by up to 2^-17, off a half step that it should lie on, while
+        // quotients of two bf16 that lie on none are more than 2^-16 away from it.  (Without that 63.5 became 63 in every other row.)
+        auto round8 = [&](float f) { return zero ? 0u : __float_as_uint(fmaf(f, inv, 384.0f) + (12582912.0f - 384.0f)) & 0xffu; };
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
             const int c = (v * NT + t) * 8;
