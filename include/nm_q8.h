@@ -19,8 +19,11 @@
  *
  * Not-a-number and infinity: a row whose values (or, for the norm, whose sum of
  * squares) are not finite in fp32 gets q = 0 and s = NaN, so everything computed from
- * it is NaN, and no other row is touched.  A row whose largest magnitude is below 1.5e-36
- * (127 times the smallest normal fp32 number) counts as zero: q = 0, s = 0.
+ * it is NaN, and no other row is touched.  A row whose largest magnitude (for the norm:
+ * that of v) is below 1.5e-36 (127 times the smallest normal fp32 number) counts as
+ * zero: q = 0, s = 0.  A norm divides by sqrt(mean(h^2) + eps), held to fp32 precision down
+ * to 1.5e-36 (2^-119); a row for which it is below that, as for a zero row with eps = 0,
+ * has no norm: q = 0, s = NaN.
  */
 #ifndef NM_Q8_H
 #define NM_Q8_H

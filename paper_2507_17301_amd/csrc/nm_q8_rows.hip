@@ -57,7 +57,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
 {
     constexpr int ES = Elem<BF16>::kBytes, BLOCK = NT < 256 ? 256 : NT, RPB = BLOCK / NT;
     constexpr bool EARLY = VPT <= 2;
-    __shared__ float psum[NT / 64];
+    __shared__ float psum[NORM ? 2 : 1][NT / 64];   // (the second sum of a row whose first is too small)
     __shared__ unsigned pmax[2][NT / 64];   // in turn: a wavefront may still read one row's when another writes the next row's
     int turn = 0;
     const int t = threadIdx.x % NT;
@@ -110,14 +110,30 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
                 }
                 if (t < over) gx = p.gamma[whole + t];
             }
-            float sum = hx * hx;
+            auto squares = [&] {
+                float sum = hx * hx;
 #pragma unroll
-            for (int v = 0; v < VPT; ++v)
+                for (int v = 0; v < VPT; ++v)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(h[v][e], h[v][e], sum);
-            sum = row_sum<NT>(sum, psum);
+                    for (int e = 0; e < 8; ++e) sum = fmaf(h[v][e], h[v][e], sum);
+                return sum;
+            };
+            const float sum = row_sum<NT>(squares(), psum[0]);
             bad = (__float_as_uint(sum) & 0x7fffffffu) >= 0x7f800000u;
-            const float r = 1.0f / sqrtf(sum / (float)p.width + p.eps);
+            float mean = sum / (float)p.width + p.eps;
+            // Squares (and an eps) that fp32 holds in few bits or not at all: the same of h * 2^64, exact.  All threads of a row come here
+            // or none.  The limit leaves the squares that fp32 does not hold, 2^16 times 2^-150, a share of 2^-38 of the sum.
+            if (mean < 0x1p-80f) {
+                constexpr float kUp = 0x1p64f;
+#pragma unroll
+                for (int v = 0; v < VPT; ++v)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) h[v][e] *= kUp;
+                hx *= kUp;
+                mean = row_sum<NT>(squares(), psum[1]) / (float)p.width + p.eps * kUp * kUp;
+                bad = mean < 0x1p-110f;   // a root mean square below 2^-119
+            }
+            const float r = 1.0f / sqrtf(mean);
 #pragma unroll
             for (int v = 0; v < VPT; ++v)
 #pragma unroll

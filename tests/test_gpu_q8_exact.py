@@ -5,6 +5,7 @@ import torch
 
 from paper_2507_17301_amd import binding as nm
 from gpu_util import say
+from q8_util import check_rounded
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +43,35 @@ def test_rounding_of_bf16_values_is_to_the_nearest_ties_to_even(dtype):
         assert not off.any(), f"{int(off.sum())} of {off.numel()}, first {xs[off][0]} in row {int(off.nonzero()[0, 0])}: {q.cpu()[off][0]} for {want[off][0]}"
         # channels of weights are rounded the same way
         assert np.array_equal(nm.nm_q8_export(nm.nm_q8_pack(xs.cuda()))[0], want.numpy())
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("width", [3, 300, 700, 1500, 4096, 5001, 20000])
+def test_norm_of_rows_whose_squares_fp32_does_not_hold(width, dtype):
+    """With no eps, or a tiny one, a norm does not depend on the magnitude of the row.  Bound: that of q8_util for the norm, 1e-5."""
+    g = torch.Generator().manual_seed(width)
+    x = torch.randn((12, width), generator=g)
+    x[:, width // 2] = 5.0
+    x *= torch.tensor([1e-8, 1e-11, 1e-13, 1e-18, 1e-20, 1e-21, 1e-22, 1e-23, 1e-26, 1e-30, 1e-34, 4e-36])[:, None]
+    x = x.to(TYPES[dtype])
+    gamma = 1 + 0.2 * torch.randn(width, generator=g)
+    for eps in (0.0, 1e-44, 1e-40, 1e-24):
+        e32 = float(np.float32(eps))
+        for r in (None, x.flip(1).contiguous()):
+            say(f"tiny rows of {width} {dtype} eps {eps} residual {r is not None}")
+            q, s, _ = nm.nm_rmsnorm_q8(x.cuda(), gamma.cuda(), None if r is None else r.cuda(), eps)
+            h = (x.float() if r is None else x.float() + r.float()).double().numpy()
+            v = gamma.double().numpy() * h / np.sqrt((h ** 2).mean(axis=1, keepdims=True) + e32)
+            check_rounded(q, s, v, 1e-5)
+    # one that is zero, or whose root mean square is below 1.5e-36, has none; its neighbours are not touched
+    x[1], x[4], x[7] = 0, 1e-38, 0
+    q, s, _ = nm.nm_rmsnorm_q8(x.cuda(), gamma.cuda(), None, 0.0)
+    h = x.double().numpy()
+    for i in range(12):
+        if i in (1, 4, 7):
+            assert torch.isnan(s[i]) and not q[i].any()
+        else:
+            check_rounded(q[i:i + 1], s[i:i + 1], gamma.double().numpy() * h[i:i + 1] / np.sqrt((h[i:i + 1] ** 2).mean()), 1e-5)
+    # with an eps above that, they are zero rows or tiny ones
+    q, s, _ = nm.nm_rmsnorm_q8(x.cuda(), gamma.cuda(), None, 1e-30)
+    assert s[1] == 0 and s[7] == 0 and not q[1].any() and not q[7].any() and torch.isfinite(s).all()
