@@ -426,6 +426,7 @@ def nm_variant_legal(v: int, wp: Packed, x_dtype: int = NM_F32, y_dtype: int = N
 # ---------------------------------------------------------------- 8-bit feed-forward operators (nm_q8.h)
 # A single token's call runs for a few us on the GPU, so these keep what they ask of a tensor short, and do not look at outputs
 # that they have allocated themselves.  A given stream is made the current one for the call: what is allocated then belongs to it.
+# All tensors lie on the current device (or the given stream's).
 def _rows_of(t, name: str):
     """(rows, width, row stride) of a device tensor whose last axis is the row: two axes with any row stride, or any
     number of them whose rows lie at one stride."""
@@ -487,8 +488,12 @@ def _q8_new(x, rows: int, width: int):
     return x.new_empty(x.shape[:-1] + (ld,), dtype=_torch.int8)[..., :width], ld
 
 
-def _q8_stream() -> int:
-    return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice())
+def _q8_stream(dev: int) -> int:
+    """The current stream, for tensors on device `dev`: the library launches on the current device, in no order with another's streams."""
+    current = _torch._C._cuda_getDevice()
+    if dev != current:
+        raise ValueError(f"the tensors are on device {dev}, the current device is {current}")
+    return _torch._C._cuda_getCurrentRawStream(dev)
 
 
 _ROWS_ARGS = struct.Struct("15qd")       # nm_rows_q8_args_t
@@ -523,7 +528,7 @@ def _q8_rows(norm: bool, x, gamma, residual, eps, q, scales, residual_out):
         if scales.shape != x.shape[:-1]:
             raise ValueError(f"scales must have the shape {tuple(x.shape[:-1])}")
         sptr = _q8_vector(scales, "scales", rows, dev)
-    rc = L.nm_rows_q8_args(_ROWS_ARGS.pack(x.data_ptr(), rptr, gptr, optr, q.data_ptr(), sptr, _q8_stream(), code, rows, width, ld, ldr, ldo,
+    rc = L.nm_rows_q8_args(_ROWS_ARGS.pack(x.data_ptr(), rptr, gptr, optr, q.data_ptr(), sptr, _q8_stream(dev), code, rows, width, ld, ldr, ldo,
                                            ldq, norm, eps))
     if rc < 0:
         _check(rc)
@@ -565,7 +570,7 @@ def nm_dequantize_q8(q, scales, dtype=None, y=None, stream=None):
     else:
         dtype = dtype or y.dtype
         ldy = _q8_stride(y, "y", q.shape, dtype, dev)
-    rc = L.nm_dequantize_q8_args(_DEQUANTIZE_ARGS.pack(q.data_ptr(), _q8_vector(scales, "scales", rows, dev), y.data_ptr(), _q8_stream(),
+    rc = L.nm_dequantize_q8_args(_DEQUANTIZE_ARGS.pack(q.data_ptr(), _q8_vector(scales, "scales", rows, dev), y.data_ptr(), _q8_stream(dev),
                                                        _q8_code(dtype, "y"), rows, width, ld, ldy))
     if rc < 0:
         _check(rc)
@@ -605,7 +610,7 @@ def nm_q8_pack(w, scales=None, gated: bool = False, stream=None) -> Q8Weights:
     channels, width, ld = _rows_of(w, "w")
     sptr = 0 if scales is None else _q8_vector(scales, "scales", channels, w.get_device())
     h = ctypes.c_void_p()
-    _check(L.nm_q8_pack(w.data_ptr(), _q8_code(w.dtype, "w"), sptr, channels, width, ld, int(bool(gated)), _q8_stream(), ctypes.byref(h)))
+    _check(L.nm_q8_pack(w.data_ptr(), _q8_code(w.dtype, "w"), sptr, channels, width, ld, int(bool(gated)), _q8_stream(w.get_device()), ctypes.byref(h)))
     return Q8Weights(h, channels, width, bool(gated))
 
 
@@ -653,7 +658,7 @@ def nm_linear_q8(q, scales, w: Q8Weights, bias=None, residual=None, dtype=None, 
             ws = q.new_empty(nbytes)
             wptr = ws.data_ptr()
     rc = L.nm_linear_q8_args(_LINEAR_ARGS.pack(qptr, _q8_vector(scales, "scales", rows, dev), handle, bptr, rptr, y.data_ptr(), wptr,
-                                               _q8_stream(), _q8_code(dtype, "y"), rows, width, ld, ldr, ldy, nbytes))
+                                               _q8_stream(dev), _q8_code(dtype, "y"), rows, width, ld, ldr, ldy, nbytes))
     if rc < 0:
         _check(rc)
     return y
