@@ -43,7 +43,8 @@ enum { NM_Q8_MAX_WIDTH = 65536 };
 /*
  * nm_quantize_q8 -- every row rounded to 8 bits under its own scale:
  *   a = max |x_i|,  s = a / 127,  q_i = x_i * 127 / a rounded to the nearest, ties to even
- *   Of bf16 values that is exact.  Of fp32 values, a quotient within 2.4e-5 of half way between two whole numbers may go to either.
+ *   Of bf16 values that is exact.  Of fp32 values, a quotient not half way between two whole numbers but within 4e-6 of
+ *   it may go to either.
  *   x_dev      rows of x_dtype (NM_F32 or NM_BF16) at stride ldx, only read
  *   q_dev      int8 rows at stride ldq >= width, fully overwritten (gaps between rows are not touched)
  *   scales_dev fp32 [rows]
@@ -63,7 +64,7 @@ int nm_dequantize_q8(const int8_t* q_dev, int64_t ldq, const float* scales_dev, 
  * nm_rmsnorm_q8 -- residual addition, root-mean-square norm and rounding to 8 bits in one pass:
  *   h = x + residual                      (h = x without one), formed in fp32
  *   v_i = gamma_i * h_i / sqrt(mean_i(h_i^2) + eps)
- *   q, s = the row v rounded as by nm_quantize_q8
+ *   q, s = the row v rounded as by nm_quantize_q8 (q: to the nearest within the fp32 errors of v)
  *   residual_out = h rounded to x_dtype   (the residual stream that the next layer adds to)
  * The norm is taken of h before that rounding; sums are fp32.
  *   residual_dev      rows of x_dtype at stride ldr, or NULL

@@ -1,6 +1,6 @@
 // Row operators in 8 bits: residual addition + root-mean-square norm + rounding, rounding alone, reading back.
 //
-//   h = x + r;  v = gamma * h / sqrt(mean(h^2) + eps);  s = max|v| / 127;  q = rint(v * 127 / max|v|), ties to even
+//   h = x + r;  v = gamma * h / sqrt(mean(h^2) + eps);  s = max|v| / 127;  q = rint(v * 127 / max|v|)
 //
 // Bound by HBM: a value is read once (twice with a residual), kept in registers over both reductions (sum of
 // squares, largest magnitude), and written once.  NT threads share a row, 8 adjacent values a thread at a time,
@@ -51,6 +51,30 @@ __device__ inline unsigned row_max(unsigned v, unsigned* part)
     }
     return v;
 }
+
+// x * 127 / a rounded once to fp32, so that a quotient half way between two whole numbers goes to the even one.  (x times 127 / a rounded is
+// off a half step by up to 2^-17: 63.5 became 63 under half of all bf16 magnitudes a.)
+// bf16: 127 / a in two parts, the first of 16 bits, whose product with x is exact.
+// fp32: the product with 127 / a rounded, then its rounding and that of 127 / a added.
+template <bool BF16> struct Quotient {
+    float inv, rest;
+    __device__ inline explicit Quotient(float a) : inv(127.0f / a)
+    {
+        if constexpr (BF16) {
+            inv = __uint_as_float(__float_as_uint(inv) & 0xffffff00u);
+            rest = fmaf(-inv, a, 127.0f) / a;
+        } else {
+            rest = fmaf(-inv, a, 127.0f) * (1.0f / 127.0f);
+        }
+    }
+    __device__ inline float operator()(float x) const
+    {
+#pragma clang fp contract(off)
+        const float y = x * inv;
+        if constexpr (BF16) return fmaf(x, rest, y);
+        else return y + fmaf(y, rest, fmaf(x, inv, -y));
+    }
+};
 
 template <bool BF16, int NT, int VPT, bool NORM>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
@@ -170,10 +194,12 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
         if (t == 0) p.scales[row] = bad ? __uint_as_float(0x7fc00000u) : none ? 0.0f : a / 127.0f;
         int8_t* pq = p.q + row * p.ldq;
         const bool zero = bad || none;
-        // 1.5 * 2^23 + n holds n, rounded to nearest even by the addition, in its low bits.  Before that a product is rounded to a multiple of
-        // 2^-15, the spacing of fp32 next to 384: the error of 127 / a moves it by up to 2^-17, off a half step that it should lie on, while
-        // quotients of two bf16 that lie on none are more than 2^-16 away from it.  (Without that 63.5 became 63 in every other row.)
-        auto round8 = [&](float f) { return zero ? 0u : __float_as_uint(fmaf(f, inv, 384.0f) + (12582912.0f - 384.0f)) & 0xffu; };
+        // 1.5 * 2^23 + n holds n, rounded to nearest even by the addition, in its low bits.  (A norm's values are themselves rounded ones.)
+        const Quotient<BF16> quotient(a);
+        auto round8 = [&](float f) {
+            if constexpr (NORM) return zero ? 0u : __float_as_uint(fmaf(f, inv, 12582912.0f)) & 0xffu;
+            else return zero ? 0u : __float_as_uint(quotient(f) + 12582912.0f) & 0xffu;
+        };
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
             const int c = (v * NT + t) * 8;

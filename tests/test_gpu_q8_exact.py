@@ -75,3 +75,30 @@ def test_norm_of_rows_whose_squares_fp32_does_not_hold(width, dtype):
     # with an eps above that, they are zero rows or tiny ones
     q, s, _ = nm.nm_rmsnorm_q8(x.cuda(), gamma.cuda(), None, 1e-30)
     assert s[1] == 0 and s[7] == 0 and not q[1].any() and not q[7].any() and torch.isfinite(s).all()
+
+
+def test_rounding_of_fp32_values_next_to_half_steps():
+    """Quotients x * 127 / a on both sides of every half step, and on it.  To the even number on it; to the nearest, except where the quotient
+    rounded to fp32 lies on the half step, within half its spacing under 128: 2^-18."""
+    rng = np.random.default_rng(3)
+    a = np.concatenate([(1 + rng.random(60)).astype(np.float32), np.float32([1, 1.5, 127, 254, 3, 1.9999999, 1e-36 * 1.6, 3e38, 1e30])])
+    near = ((np.arange(127) + 0.5) * a[:, None].astype(np.longdouble) / 127).astype(np.float32)     # [rows, 127]
+    x = near
+    for up in (np.float32(np.inf), np.float32(-np.inf)):
+        y = near
+        for _ in range(24):
+            y = np.nextafter(y, up)
+            x = np.concatenate([x, y], axis=1)
+    x = np.concatenate([x, -x, rng.uniform(-1, 1, (len(a), 4000)).astype(np.float32) * a[:, None], a[:, None]], axis=1)
+    x = np.where(np.abs(x) <= a[:, None], x, np.float32(0))
+    v = np.abs(x.astype(np.longdouble)) * 127 / a[:, None].astype(np.longdouble)
+    low = np.floor(v)
+    tie = 2 * 127 * np.abs(x.astype(np.longdouble)) == (2 * low + 1) * a[:, None].astype(np.longdouble)     # (exact: 32 bits)
+    assert tie.sum() > 300
+    nearest = np.where(tie, low + low % 2, np.rint(v))
+    say(f"fp32 values next to half steps, {x.shape}")
+    q, _ = nm.nm_quantize_q8(torch.from_numpy(x).cuda())
+    q = q.cpu().numpy().astype(np.int32)
+    assert (q * np.sign(x) >= 0).all()
+    off = (np.abs(q) != nearest) & (tie | (np.abs(v - low - 0.5) > 2.0 ** -18)) | (np.abs(np.abs(q) - nearest) > 1)
+    assert not off.any(), f"{off.sum()} of {off.size}, first {x[off][0]!r} in a row of {a[np.argwhere(off)[0, 0]]!r}: {q[off][0]}"
