@@ -112,8 +112,8 @@ int nm_q8_export(const nm_q8_t* w, int8_t* w_host, float* scales_host);
  *   y_rc = z_rc / (1 + exp(-z_rc)) * z_r,(c+C)   gated weights of 2 C channels (no residual)
  * rounded to nearest even once if y_dtype is NM_BF16.  The result does not depend on the
  * other rows of the call nor on how the sum was divided.
- *   q_dev, ldq      int8 rows of the weights' width at any stride >= 0, any alignment.  The aligned 16 bytes that hold a
- *                   row's last value are read as a whole.
+ *   q_dev, ldq      int8 rows of the weights' width at any stride >= 0, any alignment.  Gaps between rows may be read too, and so are
+ *                   the aligned 16 bytes that hold the last row's last value; what they hold changes no result.
  *   scales_dev      fp32 [rows]
  *   bias_dev        fp32 [channels] (gated: gates first, as the weights), or NULL
  *   residual_dev    rows of y_dtype at stride ldr, or NULL.  It may be y_dev itself (same stride).

@@ -384,7 +384,7 @@ int nm_linear_q8(const int8_t* q, int64_t rows, int width, int64_t ldq, const fl
     p.groups = w->groups;
     p.kblocks = w->kblocks;
     p.y_bf16 = dt == NM_BF16;
-    // 8192 x 4096 -> 16384 (268 MB) 422 us past the cache and 455 through it, 4096 x 4096 -> 24576 (201 MB) 323 and 340;
+    // In turn on one card: 8192 x 4096 -> 16384 (268 MB) 422 us past the cache and 455 through it, 4096 x 4096 -> 24576 (201 MB) 323 and 340;
     // 16384 x 1024 -> 4096 (134 MB) 89 and 83
     p.past = (size_t)rows * outs * es > ((size_t)160 << 20);
     const Q8Plan plan = q8_plan(p);

@@ -109,10 +109,11 @@ __global__ __launch_bounds__(NW * 64) void q8_few_kernel(Q8Linear p)
 // K goes by in steps of 128.  LDS holds NSW steps' weights and NSQ steps' rows, loaded straight into it: while a step is multiplied, the
 // next one's lie there and later ones' are on their way.  Operands are read from LDS half a step ahead, into the other half of
 // the operand registers, so one barrier a step is enough.  Three stages of each where they fit a CU's LDS; where they do not, two of
-// the rows and three of the weights (8192 x 4096 -> 16384 442 us with two of each, 435 with a third of the weights, 437 of the rows).
-// Bound by the power limit on large products: 8192 x 4096 -> 16384 takes 430 us, 2.56 POP/s, at 1.86 GHz with the matrix
-// units busy 64 % of the cycles; the 256 x 256 loop without any load or barrier takes 1.16 us a step on such values (0.91 on
-// zeros, 0.85 at 2.4 GHz by the instruction's 16 cycles), with them 1.38 (0.98).
+// the rows and three of the weights (8192 x 4096 -> 16384 with two of each 1.6 % slower, with a third of the rows 0.5 %).
+// Bound by the power limit on large products, and by the starts and ends of their rounds: 8192 x 4096 -> 16384 takes 422 us, 2.6 POP/s (405 to
+// 450 by the card), at 1.87 GHz with the matrix units busy 64 % of the cycles.  The 256 x 256 loop without any load or barrier takes 1.16 us a
+// step on such values (0.91 on zeros, 0.85 at 2.4 GHz by the instruction's 16 cycles), with them 1.38 (0.98): 32 steps of 8 rounds are
+// 353 us of it.  The rest is what 8 rounds take to fill the first stages and to store, with one workgroup a CU and nothing beside it.
 // Weights lie in LDS as in memory (a wavefront's operand is 1 KiB of adjacent bytes); a row's 128 bytes are 8 chunks of 16,
 // chunk c stored at c ^ (row & 7), so that the 8 rows that an LDS cycle reads lie in 8 different places.
 // SPLIT: a workgroup takes `per` of the K steps and stores its integer sums as they lie in the registers,
@@ -349,7 +350,8 @@ int launch_few(const Q8Linear& p, hipStream_t s)
     return NM_OK;
 }
 
-// More channels a workgroup read q less often, fewer make more workgroups; 256 CUs want two or more each.  us at width 4096, one row,
+// More channels a workgroup read q less often, fewer make more workgroups: 256 of them at 4096 and at 8192 channels, 192 at 12288, one a CU;
+// fewer than 4096 channels leave CUs without one (K is not divided over workgroups here).  us at width 4096, one row,
 // 16, 32, 64 rows, with 1 / 2 / 4 blocks of channels a workgroup:
 //    4096 channels   5.7 / 5.8 /  7.8    5.7 / 6.5 /  8.5     6.5 /  7.8 / 10.1     8.7 / 10.0 / 12.9
 //    8192            8.8 / 8.8 /  8.4    8.9 / 8.8 /  8.9    10.4 /  9.3 / 10.4    14.7 / 10.8 / 13.3

@@ -9,7 +9,8 @@
 // Rows of odd widths and strides run the same code (global memory takes a 16-byte access at any address); only what a
 // width leaves past its last group of 8 is taken value by value, one value a thread.
 // Sums, norm and products are fp32; the one rounding to fewer bits is that to q, of the unrounded h.
-// 16384 rows of 8192 in bf16 with a residual: 189 us, 940 MB, 5.0 TB/s (a copy of 1 GiB reaches 5.1).
+// 16384 rows of 8192 in bf16 with a residual: 185 us, 940 MB, 5.1 TB/s (a copy of 1 GiB reaches as much); in fp32, 16384 of 5001 with a
+// residual 226 us, 4.7 TB/s, and without one 112 us, 3.7: 512 x 2 groups leave 39 % of the slots empty there.
 #include "nm_q8_device.h"
 
 namespace nm {
@@ -146,7 +147,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void q8_rows_kernel(RowArgs p)
             bad = (__float_as_uint(sum) & 0x7fffffffu) >= 0x7f800000u;
             float mean = sum / (float)p.width + p.eps;
             // Squares (and an eps) that fp32 holds in few bits or not at all: the same of h * 2^64, exact.  All threads of a row come here
-            // or none.  The limit leaves the squares that fp32 does not hold, 2^16 times 2^-150, a share of 2^-38 of the sum.
+            // or none.  Partial sums are off by 2^-150 each at most where fp32 no longer holds them in full: a share of 2^-70 at this limit.
             if (mean < 0x1p-80f) {
                 constexpr float kUp = 0x1p64f;
 #pragma unroll
@@ -258,7 +259,8 @@ int launch_rows(const RowArgs& p, hipStream_t s)
 //   rounding  4096   256 x 2  2.6   37     512 x 1  2.6   39    1024 x 1  2.7   65
 //             8192   512 x 2  2.6   69     256 x 4  2.9   73    1024 x 1  2.7   84
 //            16384  1024 x 2  3.0  134     256 x 8  3.9  144     512 x 4  3.1  145
-// (16384 rows: 5.0 to 5.4 TB/s for the norm, 5.5 to 6.0 for the rounding, whose rows partly come from the last-level cache.)
+// (16384 rows: 5.0 to 5.4 TB/s for the norm, 5.5 to 6.0 for the rounding, whose rows partly come from the last-level cache.  The rounding's
+// figures are with one multiplication a value; Quotient's adds 0 to 3 %, 4 % at 512 values a row.)
 template <bool BF16, bool NORM>
 int pick_rows(const RowArgs& p, hipStream_t s)
 {
