@@ -1,6 +1,6 @@
 """ctypes binding of libnmconv.so -- argument marshalling only.
 
-Same names as the C ABI in ``include/nm_conv.h`` and ``include/nm_q8.h``.  Tensors are torch tensors
+Same names as the C ABI in ``include/nm_conv.h``, ``nm_q8.h``, ``nm_mx4.h`` and ``nm_experts.h``.  Tensors are torch tensors
 used purely as device buffers (``data_ptr()``) and for the current stream; all
 arithmetic happens inside the library's kernels.  There is no fallback: if the
 library is missing or a call fails, an exception is raised.
@@ -10,12 +10,14 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import numpy as np
 
-NM_F32, NM_BF16, NM_F8E4M3, NM_I8 = 0, 1, 2, 3
+NM_F32, NM_BF16, NM_F8E4M3, NM_I8, NM_MX4 = 0, 1, 2, 3, 4
 NM_Q8_MAX_WIDTH, NM_Q8_FEW_ROWS = 65536, 64
+NM_MX4_MAX_WIDTH, NM_MX4_MAX_EXPERTS, NM_MX4_FEW_ROWS = 65536, 1024, 64
+NM_ROUTE_MAX_EXPERTS, NM_ROUTE_MAX_CHOICES = 1024, 64
 NM_OK = 0
 NM_ERR_ARG, NM_ERR_SHAPE, NM_ERR_UNSUPPORTED, NM_ERR_ALLOC, NM_ERR_HIP, NM_ERR_IO = -1, -2, -3, -4, -5, -6
 _STATUS = {0: "NM_OK", -1: "NM_ERR_ARG", -2: "NM_ERR_SHAPE", -3: "NM_ERR_UNSUPPORTED",
@@ -90,6 +92,21 @@ def lib():
         L.nm_linear_q8.argtypes = [vp, i64, ci, i64, vp, vp, vp, vp, i64, vp, ci, i64, vp, st, vp]
         L.nm_rows_q8_args.argtypes = L.nm_dequantize_q8_args.argtypes = L.nm_linear_q8_args.argtypes = [ctypes.c_char_p]
         L.nm_linear_q8_workspace.argtypes = [vp, i64, i64, vp, ctypes.POINTER(st)]
+        L.nm_quantize_mx4.argtypes = [vp, ci, i64, ci, i64, vp, i64, vp, i64, vp]
+        L.nm_dequantize_mx4.argtypes = [vp, i64, vp, i64, i64, ci, vp, ci, i64, vp]
+        L.nm_rmsnorm_mx4.argtypes = [vp, ci, i64, ci, i64, vp, i64, vp, ctypes.c_double, vp, i64, vp, i64, vp, i64, vp]
+        L.nm_mx4_pack.argtypes = [vp, ci, vp, i64, ci, ci, ci, i64, ci, vp, ctypes.POINTER(vp)]
+        L.nm_mx4_free.argtypes = [vp]
+        L.nm_mx4_dims.argtypes = [vp, pi, pi, pi, pi]
+        L.nm_mx4_export.argtypes = [vp, vp, vp]
+        L.nm_linear_mx4.argtypes = [vp, i64, vp, i64, i64, ci, vp, vp, vp, i64, vp, ci, i64, vp, i64, vp, st, vp]
+        L.nm_experts_mx4.argtypes = [vp, i64, vp, i64, i64, ci, vp, vp, vp, i64, vp, vp, ci, i64, vp, i64, vp, st, vp]
+        L.nm_mx4_workspace.argtypes = [i64, vp, ci, ctypes.POINTER(st)]
+        L.nm_route.argtypes = [vp, ci, i64, ci, i64, ci, ci, vp, vp, vp, vp, vp, vp, st, vp]
+        L.nm_route_workspace.argtypes = [i64, ci, ctypes.POINTER(st)]
+        L.nm_combine.argtypes = [vp, ci, i64, i64, vp, vp, i64, ci, ci, vp, i64, vp, ci, i64, vp]
+        for name in ("nm_rows_mx4_args", "nm_dequantize_mx4_args", "nm_product_mx4_args", "nm_route_args", "nm_combine_args"):
+            getattr(L, name).argtypes = [ctypes.c_char_p]
         for name in ("nm_prune", "nm_packed_free", "nm_packed_dims", "nm_packed_indices",
                      "nm_packed_values", "nm_packed_mask", "nm_packed_scale", "nm_conv2d", "nm_conv2d_res", "nm_conv2d_static", "nm_conv2d_args",
                      "nm_maxpool2d",
@@ -97,7 +114,10 @@ def lib():
                      "nm_cache_save", "nm_cache_load", "nm_cache_clear", "nm_cache_size", "nm_workspace_free",
                      "nm_force_variant", "nm_variant_legal", "nm_quantize_q8", "nm_dequantize_q8", "nm_rmsnorm_q8",
                      "nm_q8_pack", "nm_q8_free", "nm_q8_dims", "nm_q8_export", "nm_linear_q8", "nm_linear_q8_workspace", "nm_rows_q8_args",
-                     "nm_dequantize_q8_args", "nm_linear_q8_args"):
+                     "nm_dequantize_q8_args", "nm_linear_q8_args", "nm_quantize_mx4", "nm_dequantize_mx4", "nm_rmsnorm_mx4", "nm_mx4_pack",
+                     "nm_mx4_free", "nm_mx4_dims", "nm_mx4_export", "nm_linear_mx4", "nm_experts_mx4", "nm_mx4_workspace", "nm_route",
+                     "nm_route_workspace", "nm_combine", "nm_rows_mx4_args", "nm_dequantize_mx4_args", "nm_product_mx4_args", "nm_route_args",
+                     "nm_combine_args"):
             getattr(L, name).restype = ci
         _lib = L
     return _lib
@@ -662,3 +682,307 @@ def nm_linear_q8(q, scales, w: Q8Weights, bias=None, residual=None, dtype=None, 
     if rc < 0:
         _check(rc)
     return y
+
+
+# ---------------------------------------------------------------- feed-forward operators in MX4, experts (nm_mx4.h, nm_experts.h)
+# Rows in MX4 are two uint8 tensors: codes [..., 16 B] and scales [..., B], with B = ceil(width / 32) blocks a row.
+_ROWS4_ARGS = struct.Struct("16qd")        # nm_rows_mx4_args_t
+_DEQUANTIZE4_ARGS = struct.Struct("10q")   # nm_dequantize_mx4_args_t
+_PRODUCT4_ARGS = struct.Struct("21q")      # nm_product_mx4_args_t
+_ROUTE_ARGS = struct.Struct("15q")         # nm_route_args_t
+_COMBINE_ARGS = struct.Struct("15q")       # nm_combine_args_t
+
+
+def _mx4_rows_of(q, scales, dev: int):
+    """(rows, blocks, row stride of the codes, of the scales) of rows in MX4."""
+    rows, nbytes, ldq = _rows_of(q, "q")
+    if q.dtype != _torch.uint8:
+        raise TypeError(f"q must be uint8, not {q.dtype}")
+    if nbytes % 16:
+        raise ValueError(f"rows of q have whole blocks of 16 bytes, not {nbytes} bytes")
+    return rows, nbytes // 16, ldq, _q8_stride(scales, "scales", q.shape[:-1] + (nbytes // 16,), _torch.uint8, dev)
+
+
+def _mx4_out(x, lead, width: int, q, scales, dev: int, names=("q", "scales")):
+    """(codes, scales, their strides) for rows of `width` values: those that were given, or new ones."""
+    nb = (width + 31) // 32
+    if q is None:
+        q, ldq = x.new_empty(lead + (nb * 16,), dtype=_torch.uint8), nb * 16
+    else:
+        ldq = _q8_stride(q, names[0], lead + (nb * 16,), _torch.uint8, dev)
+    if scales is None:
+        scales, lds = x.new_empty(lead + (nb,), dtype=_torch.uint8), nb
+    else:
+        lds = _q8_stride(scales, names[1], lead + (nb,), _torch.uint8, dev)
+    return q, scales, ldq, lds
+
+
+def _mx4_rows(norm: bool, x, gamma, residual, eps, q, scales, residual_out):
+    L = _lib or lib()
+    rows, width, ld = _rows_of(x, "x")
+    dtype, dev = x.dtype, x.get_device()
+    code = _q8_code(dtype, "x")
+    gptr = rptr = optr = ldr = 0
+    ldo = width
+    if gamma is not None:
+        gptr = _q8_vector(gamma, "gamma", width, dev)
+    if residual is not None:
+        ldr, rptr = _q8_stride(residual, "residual", x.shape, dtype, dev), residual.data_ptr()
+    if residual_out is not None:
+        ldo, optr = _q8_stride(residual_out, "residual_out", x.shape, dtype, dev), residual_out.data_ptr()
+    elif residual is not None:
+        residual_out = _q8_like(x, dtype)
+        optr = residual_out.data_ptr()
+    q, scales, ldq, lds = _mx4_out(x, x.shape[:-1], width, q, scales, dev)
+    rc = L.nm_rows_mx4_args(_ROWS4_ARGS.pack(x.data_ptr(), rptr, gptr, optr, q.data_ptr(), scales.data_ptr(), _q8_stream(dev), code, rows, width, ld,
+                                             ldr, ldo, ldq, lds, norm, eps))
+    if rc < 0:
+        _check(rc)
+    return q, scales, residual_out
+
+
+def nm_quantize_mx4(x, q=None, scales=None, stream=None):
+    """Rows of x (fp32 or bf16, the last axis) in MX4: (codes uint8 [..., 16 B], scales uint8 [..., B])."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return _mx4_rows(False, x, None, None, 0.0, q, scales, None)[:2]
+    return _mx4_rows(False, x, None, None, 0.0, q, scales, None)[:2]
+
+
+def nm_rmsnorm_mx4(x, gamma=None, residual=None, eps: float = 1e-6, q=None, scales=None, residual_out=None, stream=None):
+    """h = x + residual; rows of gamma * h / sqrt(mean(h^2) + eps) in MX4.  Returns (codes, scales, h rounded to x's dtype); the
+    last is None without a residual unless residual_out is given.  residual_out may be x or residual."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return _mx4_rows(True, x, gamma, residual, eps, q, scales, residual_out)
+    return _mx4_rows(True, x, gamma, residual, eps, q, scales, residual_out)
+
+
+def nm_dequantize_mx4(q, scales, width=None, dtype=None, y=None, stream=None):
+    """The values that rows in MX4 stand for, in fp32 or bf16 (`dtype`; default fp32 or y's), `width` of them (default: all of
+    the blocks', or y's)."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return nm_dequantize_mx4(q, scales, width, dtype, y)
+    L = _lib or lib()
+    dev = q.get_device()
+    rows, nb, ldq, lds = _mx4_rows_of(q, scales, dev)
+    if width is None:
+        width = nb * 32 if y is None else y.shape[-1]
+    if (width + 31) // 32 != nb:
+        raise ValueError(f"rows of {nb} blocks do not hold {width} values")
+    shape, ldy = q.shape[:-1] + (width,), width
+    if y is None:
+        dtype = dtype or _torch.float32
+        y = q.new_empty(shape, dtype=dtype)
+    else:
+        dtype = dtype or y.dtype
+        ldy = _q8_stride(y, "y", shape, dtype, dev)
+    rc = L.nm_dequantize_mx4_args(_DEQUANTIZE4_ARGS.pack(q.data_ptr(), scales.data_ptr(), y.data_ptr(), _q8_stream(dev), _q8_code(dtype, "y"), rows,
+                                                         width, ldq, lds, ldy))
+    if rc < 0:
+        _check(rc)
+    return y
+
+
+class MX4Weights:
+    """Owner of an nm_mx4_t handle: [channels, width] weights in MX4, or [experts, channels, width]."""
+
+    def __init__(self, handle, experts: int, channels: int, width: int, gated: bool):
+        self.handle = handle
+        self.experts, self.channels, self.width, self.gated = experts, channels, width, gated
+        self.blocks = (width + 31) // 32
+        self.outs = channels // 2 if gated else channels
+
+    def free(self):
+        """Release the handle now (idempotent)."""
+        h, self.handle = getattr(self, "handle", None), None
+        if h and _lib is not None:
+            _lib.nm_mx4_free(h)
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def nm_mx4_pack(w, scales=None, width=None, gated: bool = False, stream=None) -> MX4Weights:
+    """Weights [channels, width] or [experts, channels, width] on the device: fp32 / bf16, which are rounded here, or codes (uint8
+    [..., 16 B]) with scales (uint8 [..., B]) and the width that they hold (default: all of the blocks').  gated: of each
+    expert's channels the first half gates the second."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return nm_mx4_pack(w, scales, width, gated)
+    L = _lib or lib()
+    if w.dim() not in (2, 3):
+        raise ValueError("w must have two or three axes")
+    dev = w.get_device()
+    sptr = lds = 0
+    if scales is not None:
+        rows, nb, ld, lds = _mx4_rows_of(w, scales, dev)
+        code, sptr = NM_MX4, scales.data_ptr()
+        width = nb * 32 if width is None else width
+        if (width + 31) // 32 != nb:
+            raise ValueError(f"rows of {nb} blocks do not hold {width} values")
+    else:
+        rows, n, ld = _rows_of(w, "w")
+        if width is not None and width != n:
+            raise ValueError(f"w has rows of {n} values, not {width}")
+        code, width = _q8_code(w.dtype, "w"), n
+    experts, channels = w.shape[0] if w.dim() == 3 else 1, w.shape[-2]
+    h = ctypes.c_void_p()
+    _check(L.nm_mx4_pack(w.data_ptr(), code, sptr, lds, experts, channels, width, ld, int(bool(gated)), _q8_stream(dev), ctypes.byref(h)))
+    return MX4Weights(h, experts, channels, width, bool(gated))
+
+
+def nm_mx4_export(w: MX4Weights):
+    """(codes uint8 [experts, channels, 16 B], scales uint8 [experts, channels, B]) as numpy arrays."""
+    q, s = np.empty((w.experts, w.channels, w.blocks * 16), dtype=np.uint8), np.empty((w.experts, w.channels, w.blocks), dtype=np.uint8)
+    _check(lib().nm_mx4_export(w.handle, q.ctypes.data, s.ctypes.data))
+    return q, s
+
+
+def _mx4_product(q, scales, w: MX4Weights, offsets, index, bias, residual, dtype, y, y_scales, rounded: bool):
+    L = _lib or lib()
+    dev = q.get_device()
+    sources, nb, ldq, lds = _mx4_rows_of(q, scales, dev)
+    if nb != w.blocks:
+        raise ValueError(f"rows of {nb} blocks, weights of {w.blocks}")
+    optr = iptr = bptr = rptr = ldr = sptr = ldys = 0
+    rows, outs = sources, w.outs
+    lead = q.shape[:-1]
+    if offsets is not None:
+        optr = _int_vector(offsets, "offsets", w.experts + 1, dev)
+        if index is not None:
+            rows = index.numel()
+            iptr = _int_vector(index, "index", rows, dev)
+            lead = (rows,)
+    shape, ldy = lead + (outs,), outs
+    if rounded:
+        y, y_scales, ldy, ldys = _mx4_out(q, lead, outs, y, y_scales, dev, ("y", "y_scales"))
+        code, sptr = NM_MX4, y_scales.data_ptr()
+    else:
+        if y_scales is not None:
+            raise ValueError("y_scales belong to an output in MX4")
+        if y is None:
+            dtype = dtype or _torch.bfloat16
+            y = q.new_empty(shape, dtype=dtype)
+        else:
+            dtype = dtype or y.dtype
+            ldy = _q8_stride(y, "y", shape, dtype, dev)
+        code = _q8_code(dtype, "y")
+    if bias is not None:
+        bptr = _q8_vector(bias, "bias", w.experts * w.channels, dev)
+    if residual is not None:
+        ldr, rptr = _q8_stride(residual, "residual", shape, y.dtype, dev), residual.data_ptr()
+    handle = w.handle.value if w.handle else 0
+    wptr = nbytes = 0
+    if optr or rows > NM_MX4_FEW_ROWS:   # (else none is needed)
+        need = ctypes.c_size_t(0)
+        rc = L.nm_mx4_workspace(rows, handle, 1 if optr else 0, ctypes.byref(need))
+        if rc < 0:
+            _check(rc)
+        nbytes = need.value
+        if nbytes:
+            ws = q.new_empty(nbytes)
+            wptr = ws.data_ptr()
+    rc = L.nm_product_mx4_args(_PRODUCT4_ARGS.pack(q.data_ptr(), scales.data_ptr(), handle, bptr, rptr, optr, iptr, y.data_ptr(), sptr, wptr,
+                                                   _q8_stream(dev), code, sources, w.width, ldq, lds, ldr, rows, ldy, ldys, nbytes))
+    if rc < 0:
+        _check(rc)
+    return (y, y_scales) if rounded else y
+
+
+def nm_linear_mx4(q, scales, w: MX4Weights, bias=None, residual=None, dtype=None, y=None, y_scales=None, rounded: bool = False, stream=None):
+    """Rows in MX4 times weights in MX4: x @ w.T + bias + residual, or the gated form silu(gate) * up.  y: [..., channels] (gated:
+    half of them) in bf16 (default) or fp32; residual is typed and shaped like y and may be y.  rounded: the result in MX4,
+    (codes, scales)."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return _mx4_product(q, scales, w, None, None, bias, residual, dtype, y, y_scales, rounded)
+    return _mx4_product(q, scales, w, None, None, bias, residual, dtype, y, y_scales, rounded)
+
+
+def nm_experts_mx4(q, scales, w: MX4Weights, offsets, rows=None, bias=None, dtype=None, y=None, y_scales=None, rounded: bool = False, stream=None):
+    """Products grouped by expert: row r of the result, offsets[e] <= r < offsets[e + 1], is row r of x (with `rows`: row rows[r])
+    times expert e's weights, with its bias [experts, channels]; otherwise as nm_linear_mx4.  offsets [experts + 1] and rows are
+    int32 on the device, as nm_route gives them; rows of the result in no group are left as they were."""
+    if offsets is None:
+        raise ValueError("offsets must be given")
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return _mx4_product(q, scales, w, offsets, rows, bias, None, dtype, y, y_scales, rounded)
+    return _mx4_product(q, scales, w, offsets, rows, bias, None, dtype, y, y_scales, rounded)
+
+
+def _int_vector(t, name: str, n: int, dev: int) -> int:
+    """Pointer of a contiguous int32 tensor of n values on device `dev`."""
+    if t.dtype != _torch.int32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} values on device {dev}")
+    return t.data_ptr()
+
+
+class Routing(NamedTuple):
+    """What nm_route says: ids, weights and slots [tokens..., k], offsets [experts + 1], rows [tokens * k]."""
+    ids: "object"
+    weights: "object"
+    offsets: "object"
+    rows: "object"
+    slots: "object"
+
+
+def nm_route(logits, k: int, normalise: bool = True, stream=None) -> Routing:
+    """Each token's k largest of its logits [..., experts] (fp32 or bf16; ties go to the lowest expert), their softmax (over the
+    chosen, or over all experts), and the tokens in the order of the experts: expert e has the entries offsets[e] to
+    offsets[e + 1] - 1, entry i is token rows[i], and choice j of token t is entry slots[t, j].  Minus infinity closes an
+    expert: ids and slots of what is not chosen are -1, their weights 0."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return nm_route(logits, k, normalise)
+    L = _lib or lib()
+    tokens, experts, ld = _rows_of(logits, "logits")
+    dev, lead = logits.get_device(), logits.shape[:-1]
+    i32 = _torch.int32
+    ids, weights, slots = (logits.new_empty(lead + (k,), dtype=t) for t in (i32, _torch.float32, i32))
+    offsets, rows = logits.new_empty((experts + 1,), dtype=i32), logits.new_empty((tokens * k,), dtype=i32)
+    need = ctypes.c_size_t(0)
+    _check(L.nm_route_workspace(tokens, experts, ctypes.byref(need)))
+    ws = logits.new_empty(need.value, dtype=_torch.uint8) if need.value else None
+    rc = L.nm_route_args(_ROUTE_ARGS.pack(logits.data_ptr(), ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(),
+                                          0 if ws is None else ws.data_ptr(), _q8_stream(dev), _q8_code(logits.dtype, "logits"), tokens, experts, ld, k,
+                                          bool(normalise), need.value))
+    if rc < 0:
+        _check(rc)
+    return Routing(ids, weights, offsets, rows, slots)
+
+
+def nm_combine(y, slots, weights, residual=None, dtype=None, out=None, stream=None):
+    """out[t] = residual[t] + sum over j of weights[t, j] * y[slots[t, j]], summed in fp32.  slots (int32, -1 adds nothing) and
+    weights (fp32) [..., k]; out [..., width] in residual's dtype, `dtype` or y's; it may be residual."""
+    if stream is not None:
+        with _lib_torch().cuda.stream(stream):
+            return nm_combine(y, slots, weights, residual, dtype, out)
+    L = _lib or lib()
+    if y.dim() != 2:
+        raise ValueError("y must have two axes")
+    entries, width, ldy = _rows_of(y, "y")
+    dev, lead, k = y.get_device(), slots.shape[:-1], slots.shape[-1]
+    if weights.shape != slots.shape:
+        raise ValueError(f"weights must have the shape {tuple(slots.shape)}")
+    n = slots.numel()
+    shape, ldo, rptr, ldr = lead + (width,), width, 0, 0
+    if out is not None:
+        dtype = dtype or out.dtype
+        ldo = _q8_stride(out, "out", shape, dtype, dev)
+    else:
+        dtype = dtype or (y.dtype if residual is None else residual.dtype)
+        out = y.new_empty(shape, dtype=dtype)
+    if residual is not None:
+        ldr, rptr = _q8_stride(residual, "residual", shape, dtype, dev), residual.data_ptr()
+    rc = L.nm_combine_args(_COMBINE_ARGS.pack(y.data_ptr(), _int_vector(slots, "slots", n, dev), _q8_vector(weights, "weights", n, dev), rptr, out.data_ptr(),
+                                              _q8_stream(dev), _q8_code(y.dtype, "y"), entries, ldy, lead.numel(), k, width, ldr, _q8_code(dtype, "out"),
+                                              ldo))
+    if rc < 0:
+        _check(rc)
+    return out

@@ -151,7 +151,8 @@ def _shapes_wave():
 def _jobs():
     jobs = []
     for src in ("nm_api.hip", "nm_prune_kernels.hip", "nm_pool_kernels.hip", "nm_conv_registry.hip", "nm_scratch.hip",
-                "nm_q8_api.hip", "nm_q8_rows.hip", "nm_q8_linear.hip"):
+                "nm_q8_api.hip", "nm_q8_rows.hip", "nm_q8_linear.hip",
+                "nm_mx4_api.hip", "nm_mx4_rows.hip", "nm_mx4_product.hip", "nm_experts.hip"):
         jobs.append((os.path.join(CSRC, src), os.path.join(OBJDIR, src.replace(".hip", ".o")), []))
     inst = os.path.join(CSRC, "nm_conv_inst.hip")
     for nb, wp, nj in _shapes():
@@ -218,9 +219,12 @@ def _jobs():
     return jobs
 
 
-def _newest_header(q8=False):
-    """Time of the last change to a header; the headers of the 8-bit operators (nm_q8*) count for their own sources only."""
-    hs = [os.path.join(d, f) for d in (CSRC, INCLUDE) for f in os.listdir(d) if f.endswith(".h") and (q8 or not f.startswith("nm_q8"))]
+_FEEDFORWARD = ("nm_q8", "nm_mx4", "nm_experts", "nm_rows_checks")   # sources and headers of the feed-forward operators
+
+
+def _newest_header(feedforward=False):
+    """Time of the last change to a header; those of the feed-forward operators count for their own sources only."""
+    hs = [os.path.join(d, f) for d in (CSRC, INCLUDE) for f in os.listdir(d) if f.endswith(".h") and (feedforward or not f.startswith(_FEEDFORWARD))]
     return max(os.path.getmtime(h) for h in hs)
 
 
@@ -243,10 +247,10 @@ def build(jobs: int = 8, force: bool = True) -> str:
     """Compile every translation unit and link libnmconv.so.  With force=False
     only out-of-date objects are rebuilt."""
     os.makedirs(OBJDIR, exist_ok=True)
-    hdr_time = {q8: _newest_header(q8) for q8 in (False, True)}
+    hdr_time = {ff: _newest_header(ff) for ff in (False, True)}
     todo = _jobs()
     with ThreadPoolExecutor(max_workers=max(1, jobs)) as ex:
-        objs = list(ex.map(lambda j: _compile(j, force, hdr_time[os.path.basename(j[0]).startswith("nm_q8")]), todo))
+        objs = list(ex.map(lambda j: _compile(j, force, hdr_time[os.path.basename(j[0]).startswith(_FEEDFORWARD)]), todo))
     cmd = [HIPCC, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:

@@ -1,0 +1,351 @@
+// Routing of tokens to experts, and the weighted sum of what the experts answer.
+#include "nm_mx4_device.h"
+
+namespace nm {
+namespace {
+
+// ---------------------------------------------------------------- routing
+// Tokens go by in chunks, one a workgroup, a chunk in batches of 64.  A token belongs to L lanes, which hold its logits as whole numbers
+// that sort like them; its choices are taken one after another, each the largest of (logit, lowest expert) over the lanes.
+// The order by expert comes of one 64-bit mask an expert and batch, with a bit for each token that chose it: an expert's count is the number of
+// its bits, a token's place among the batch's the number of bits below its own.  So no order of atomics shows in a result.
+constexpr int kThreads = 1024, kBatch = 64, kChunks = 256;
+
+template <int CTRL> __device__ inline unsigned dpp(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+
+struct Best {
+    unsigned key, expert;
+    __device__ inline void take(unsigned k, unsigned e)
+    {
+        const bool other = k > key || (k == key && e < expert);
+        key = other ? k : key;
+        expert = other ? e : expert;
+    }
+};
+
+template <int L> __device__ inline Best best_of(Best b)
+{
+    b.take(dpp<0xb1>(b.key), dpp<0xb1>(b.expert));     // lane ^ 1
+    b.take(dpp<0x4e>(b.key), dpp<0x4e>(b.expert));     // lane ^ 2
+    b.take(dpp<0x141>(b.key), dpp<0x141>(b.expert));   // mirrored in eight
+    b.take(dpp<0x140>(b.key), dpp<0x140>(b.expert));   // mirrored in sixteen
+    if constexpr (L == 64) {
+        b.take(__shfl_xor(b.key, 16), __shfl_xor(b.expert, 16));
+        b.take(__shfl_xor(b.key, 32), __shfl_xor(b.expert, 32));
+    }
+    return b;
+}
+
+template <int L> __device__ inline float sum_of(float v)
+{
+    for (int m = 1; m < L; m <<= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+constexpr unsigned kClosed = 0x007fffffu;   // the key of minus infinity; no open expert has one as small
+
+// 0 and -0 are the same, a NaN is more than infinity.
+__device__ inline unsigned key_of(float f)
+{
+    if (f != f) return 0xffffffffu;
+    const unsigned u = __float_as_uint(f + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ inline float logit_of(unsigned key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+
+// Chooses for the tokens of one batch; their bits go into mask.
+template <int L, int V>
+__device__ inline void choose(const Route& r, int64_t first, int count, unsigned long long* mask)
+{
+    constexpr int PER = kThreads / L, SLOTS = NM_ROUTE_MAX_CHOICES / L;   // tokens at a time; choices a lane keeps
+    const int l = threadIdx.x % L;
+    for (int t = threadIdx.x / L; t < count; t += PER) {
+        const int64_t token = first + t;
+        unsigned key[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = v * L + l;
+            key[v] = 0;
+            if (e < r.experts) {
+                const int64_t at = token * r.ld + e;
+                key[v] = key_of(r.bf16 ? Elem<true>::load1((const char*)r.logits + at * 2) : Elem<false>::load1((const char*)r.logits + at * 4));
+            }
+        }
+        float top = 0.0f, sum = 0.0f, p[SLOTS];
+        int id[SLOTS];
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) { p[s] = 0.0f; id[s] = -1; }
+        for (int j = 0; j < r.choices; ++j) {
+            Best b{0, 0xffffffffu};
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const bool more = key[v] > b.key;   // (a lane's experts rise with v)
+                b.key = more ? key[v] : b.key;
+                b.expert = more ? v * L + l : b.expert;
+            }
+            b = best_of<L>(b);
+            if (b.key <= kClosed) break;   // (the same for all lanes of a token)
+            const float logit = logit_of(b.key);
+            if (j == 0) {
+                top = logit;
+                if (!r.normalise) {
+                    float part = 0.0f;
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        if (key[v] > kClosed) part += expf(logit_of(key[v]) - top);
+                    sum = sum_of<L>(part);
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (b.expert == (unsigned)(v * L + l)) key[v] = 0;
+            const float e = expf(logit - top);
+            if (r.normalise) sum += e;
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s)
+                if (j == s * L + l) { p[s] = e; id[s] = (int)b.expert; }
+        }
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            const int j = s * L + l;
+            if (j < r.choices) {
+                const int64_t at = token * r.choices + j;
+                r.ids[at] = id[s];
+                r.weights[at] = id[s] < 0 ? 0.0f : p[s] / sum;
+                if (id[s] >= 0) atomicOr(&mask[id[s]], 1ull << t);
+            }
+        }
+    }
+}
+
+// Gives a batch's choices their entries; base: an expert's first entry for this batch.
+__device__ inline void place(const Route& r, int64_t first, int count, const unsigned long long* mask, const int* base)
+{
+    for (int i = threadIdx.x; i < count * r.choices; i += kThreads) {
+        const int t = i / r.choices;
+        const int64_t at = first * r.choices + i;
+        const int e = r.ids[at];
+        int slot = -1;
+        if (e >= 0) {
+            slot = base[e] + __popcll(mask[e] & ((1ull << t) - 1));
+            r.rows[slot] = (int)(first + t);
+        }
+        r.slots[at] = slot;
+    }
+}
+
+// Entries past the last one, by all workgroups together.
+__device__ inline void clear_rows(const Route& r, int from)
+{
+    for (int64_t i = from + (int64_t)blockIdx.x * kThreads + threadIdx.x; i < r.tokens * r.choices; i += (int64_t)gridDim.x * kThreads) r.rows[i] = -1;
+}
+
+struct Shared {
+    unsigned long long mask[NM_ROUTE_MAX_EXPERTS];
+    int base[NM_ROUTE_MAX_EXPERTS + 1];
+    int part[kThreads];
+    int waves[kThreads / 64];
+};
+
+// base[e] becomes the sum of base[0 .. e - 1]; returns the sum of all.
+__device__ inline int scan(Shared& s, int experts)
+{
+    const int t = threadIdx.x, lane = t & 63;
+    const int mine = t < experts ? s.base[t] : 0;
+    int v = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(v, d);
+        if (lane >= d) v += up;
+    }
+    if (lane == 63) s.waves[t >> 6] = v;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kThreads / 64; ++w) {
+        before += w < (t >> 6) ? s.waves[w] : 0;
+        all += s.waves[w];
+    }
+    if (t < experts) s.base[t] = before + v - mine;
+    __syncthreads();
+    return all;
+}
+
+// All that there is to do where the tokens are one batch; otherwise the choices and each chunk's counts.
+template <int L, int V>
+__global__ __launch_bounds__(kThreads) void route_choose_kernel(Route r, int chunk, int* counts)
+{
+    __shared__ Shared s;
+    const int64_t first = (int64_t)blockIdx.x * chunk;
+    const int64_t end = first + chunk < r.tokens ? first + chunk : r.tokens;
+    const int e = threadIdx.x;
+    int total = 0;
+    for (int64_t at = first; at < end || at == first; at += kBatch) {
+        if (e < r.experts) s.mask[e] = 0;
+        __syncthreads();
+        const int count = (int)(end - at < kBatch ? (end > at ? end - at : 0) : kBatch);
+        choose<L, V>(r, at, count, s.mask);
+        __syncthreads();
+        if (e < r.experts) total += __popcll(s.mask[e]);
+    }
+    if (counts) {
+        if (e < r.experts) counts[(int64_t)blockIdx.x * r.experts + e] = total;
+        return;
+    }
+    if (e < r.experts) s.base[e] = total;
+    __syncthreads();
+    const int all = scan(s, r.experts);
+    if (e < r.experts) r.offsets[e] = s.base[e];
+    if (e == 0) r.offsets[r.experts] = all;
+    place(r, 0, (int)r.tokens, s.mask, s.base);
+    clear_rows(r, all);
+}
+
+// The entries of one chunk: its first for each expert come after those of the experts and the chunks before.
+__global__ __launch_bounds__(kThreads) void route_place_kernel(Route r, int chunk, const int* counts)
+{
+    __shared__ Shared s;
+    const int t = threadIdx.x, chunks = gridDim.x, mine = blockIdx.x;
+    int pad = 64;
+    while (pad < r.experts) pad <<= 1;   // threads of a part: the chunks are dealt to kThreads / pad of them
+    const int parts = kThreads / pad, part = t / pad, e = t % pad;
+    int all = 0, before = 0;
+    if (e < r.experts) {
+#pragma unroll 8
+        for (int c = part; c < chunks; c += parts) {
+            const int n = counts[(int64_t)c * r.experts + e];
+            all += n;
+            before += c < mine ? n : 0;
+        }
+    }
+    s.part[t] = all;
+    __syncthreads();
+    if (t < r.experts) {
+        int n = 0;
+        for (int i = 0; i < parts; ++i) n += s.part[i * pad + t];
+        s.base[t] = n;
+    }
+    __syncthreads();
+    s.part[t] = before;
+    const int entries = scan(s, r.experts);
+    if (mine == 0) {
+        if (t < r.experts) r.offsets[t] = s.base[t];
+        if (t == 0) r.offsets[r.experts] = entries;
+    }
+    if (t < r.experts) {   // (after scan's last barrier, which s.part's writes precede)
+        int n = s.base[t];
+        for (int i = 0; i < parts; ++i) n += s.part[i * pad + t];
+        s.base[t] = n;
+    }
+    const int64_t first = (int64_t)mine * chunk;
+    const int64_t end = first + chunk < r.tokens ? first + chunk : r.tokens;
+    for (int64_t at = first; at < end; at += kBatch) {
+        const int count = (int)(end - at < kBatch ? end - at : kBatch);
+        if (t < r.experts) s.mask[t] = 0;
+        __syncthreads();
+        for (int i = t; i < count * r.choices; i += kThreads) {
+            const int id = r.ids[at * r.choices + i];
+            if (id >= 0) atomicOr(&s.mask[id], 1ull << (i / r.choices));
+        }
+        __syncthreads();
+        place(r, at, count, s.mask, s.base);
+        __syncthreads();
+        if (t < r.experts) s.base[t] += __popcll(s.mask[t]);
+    }
+    clear_rows(r, entries);
+}
+
+inline int chunk_of(int64_t tokens)
+{
+    const int64_t each = (tokens + kChunks - 1) / kChunks;
+    return (int)((each + kBatch - 1) / kBatch * kBatch);
+}
+
+// ---------------------------------------------------------------- combination
+// Eight adjacent values of a row a thread.  Bound by HBM: the experts' rows are read once.
+template <bool YBF16, bool BF16>
+__global__ __launch_bounds__(256) void combine_kernel(Combine p, int units)
+{
+    constexpr int YS = Elem<YBF16>::kBytes, ES = Elem<BF16>::kBytes;
+    const int64_t total = p.tokens * units;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = total <= 0xffffffffll ? (int64_t)((unsigned)i / (unsigned)units) : i / units;
+        const int c = (int)(i - row * units) * 8;
+        const bool whole = c + 8 <= p.width;
+        float sum[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+        const int* slots = p.slots + row * p.choices;
+        const float* weights = p.weights + row * p.choices;
+#pragma unroll 4
+        for (int j = 0; j < p.choices; ++j) {
+            const int slot = slots[j];
+            if (slot == -1) continue;
+            const bool there = slot >= 0 && slot < p.entries;
+            const float w = there ? weights[j] : __uint_as_float(0x7fc00000u);
+            const char* py = (const char*)p.y + (there ? slot : 0) * p.ldy * YS + (size_t)c * YS;
+            float v[8];
+            if (whole && there) {
+                Elem<YBF16>::load8(py, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = there && c + e < p.width ? Elem<YBF16>::load1(py + e * YS) : 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = fmaf(w, v[e], sum[e]);
+        }
+        char* po = (char*)p.out + (row * p.ldo + c) * ES;
+        const char* pr = p.res ? (const char*)p.res + (row * p.ldr + c) * ES : nullptr;
+        if (whole) {
+            if (pr) {
+                float r[8];
+                Elem<BF16>::load8(pr, r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += r[e];
+            }
+            Elem<BF16>::store8(po, sum);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < p.width) Elem<BF16>::store1(po + e * ES, pr ? sum[e] + Elem<BF16>::load1(pr + e * ES) : sum[e]);
+        }
+    }
+}
+
+}  // namespace
+
+size_t route_workspace(int64_t tokens, int experts)
+{
+    if (tokens <= kBatch) return 0;
+    const int chunk = chunk_of(tokens);
+    return (size_t)((tokens + chunk - 1) / chunk) * experts * sizeof(int);
+}
+
+int run_route(const Route& r, void* workspace, hipStream_t s)
+{
+    const bool one = r.tokens <= kBatch;
+    const int chunk = one ? kBatch : chunk_of(r.tokens);
+    const dim3 grid(one ? 1u : (unsigned)((r.tokens + chunk - 1) / chunk));
+    int* counts = one ? nullptr : (int*)workspace;
+    if (r.experts <= 64) hipLaunchKernelGGL((route_choose_kernel<16, 4>), grid, dim3(kThreads), 0, s, r, chunk, counts);
+    else if (r.experts <= 256) hipLaunchKernelGGL((route_choose_kernel<16, 16>), grid, dim3(kThreads), 0, s, r, chunk, counts);
+    else hipLaunchKernelGGL((route_choose_kernel<64, 16>), grid, dim3(kThreads), 0, s, r, chunk, counts);
+    NM_HIP_CHECK(hipGetLastError());
+    if (one) return NM_OK;
+    hipLaunchKernelGGL(route_place_kernel, grid, dim3(kThreads), 0, s, r, chunk, (const int*)counts);
+    NM_HIP_CHECK(hipGetLastError());
+    return NM_OK;
+}
+
+int run_combine(const Combine& c, hipStream_t s)
+{
+    const int units = (c.width + 7) / 8;
+    const int64_t blocks = (c.tokens * units + 255) / 256;
+    const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)));
+    if (c.y_bf16 && c.bf16) hipLaunchKernelGGL((combine_kernel<true, true>), grid, dim3(256), 0, s, c, units);
+    else if (c.y_bf16) hipLaunchKernelGGL((combine_kernel<true, false>), grid, dim3(256), 0, s, c, units);
+    else if (c.bf16) hipLaunchKernelGGL((combine_kernel<false, true>), grid, dim3(256), 0, s, c, units);
+    else hipLaunchKernelGGL((combine_kernel<false, false>), grid, dim3(256), 0, s, c, units);
+    NM_HIP_CHECK(hipGetLastError());
+    return NM_OK;
+}
+
+}  // namespace nm

@@ -1,0 +1,212 @@
+// Device code that the product kernels in MX4 share: the matrix instruction, which rows a tile has, the epilogue.
+#pragma once
+
+#include "nm_mx4_device.h"
+#include "nm_q8_product.h"
+
+namespace nm {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// 16 rows of weights times 16 rows of x over 128 k.  OW and OX: the byte of the scales' words that this instruction takes.
+template <int OW, int OX>
+__device__ inline f32x4 mma4(i32x4 w, i32x4 x, f32x4 acc, unsigned ws, unsigned xs)
+{
+    const i32x8 a = __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1), b = __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, OW, (int)ws, OX, (int)xs);
+}
+
+// Rows of y that a workgroup has, and whose weights they meet.
+struct RowTile {
+    int expert, count;
+    int64_t row0;
+};
+
+// Tile number `tile` of `per` rows: the groups' tiles follow one another.  Every wavefront looks for itself, 64 groups at a time.
+// count is 0 past the last group's last tile.
+__device__ inline RowTile row_tile(const Mx4Product& p, int tile, int per)
+{
+    if (!p.grouped) {
+        const int64_t row0 = (int64_t)tile * per;
+        return {0, (int)(p.rows - row0 < per ? p.rows - row0 : per), row0};
+    }
+    const int lane = threadIdx.x & 63;
+    for (int e0 = 0; e0 < p.experts; e0 += 64) {
+        const int e = e0 + lane;
+        int from = 0, n = 0;
+        if (e < p.experts) {   // (values outside the rows of y count as the nearer end)
+            from = min(max(p.offsets[e], 0), p.rows);
+            n = max(min(max(p.offsets[e + 1], 0), p.rows) - from, 0);
+        }
+        const int tiles = (n + per - 1) / per;
+        int to = tiles;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int up = __shfl_up(to, d);
+            if (lane >= d) to += up;
+        }
+        const unsigned long long past = __ballot(to > tile);
+        if (past) {
+            const int l = __ffsll(past) - 1;
+            const int in = __builtin_amdgcn_readfirstlane(tile - (__shfl(to, l) - __shfl(tiles, l)));
+            const int left = __builtin_amdgcn_readfirstlane(__shfl(n, l)) - in * per;
+            return {e0 + l, left < per ? left : per, (int64_t)__builtin_amdgcn_readfirstlane(__shfl(from, l)) + (int64_t)in * per};
+        }
+        tile -= __builtin_amdgcn_readlane(to, 63);
+    }
+    return {0, 0, 0};
+}
+
+// Where row `row` of a tile comes from: rows of x from `base` on that the kernels' buffers begin with.  -1: nowhere.
+__device__ inline int source_of(const Mx4Product& p, const RowTile& t, int row)
+{
+    if (row >= t.count) return -1;
+    if (!p.index) return row;
+    const int at = p.index[t.row0 + row];
+    return (unsigned)at < (unsigned)p.sources ? at : -2;   // -2: an index outside x
+}
+
+// The buffers of codes and scales of a tile's rows.
+struct RowBuffers {
+    __amdgpu_buffer_rsrc_t q, s;
+    __device__ inline RowBuffers(const Mx4Product& p, const RowTile& t)
+    {
+        const int64_t first = p.index ? 0 : t.row0;
+        const int64_t rows = p.index ? p.sources : t.count;
+        q = q8_rsrc(p.q + first * p.ldq, (unsigned)((rows - 1) * p.ldq + p.blocks * 16));
+        s = q8_rsrc(p.s + first * p.lds, (unsigned)((rows - 1) * p.lds + p.blocks));
+    }
+};
+
+// The two scales of a row that a lane needs in a step, as the low bytes of a word: blocks kb and kb + 1.  Past the row's blocks 1 (the
+// codes there meet zeros), for an index outside x NaN.
+__device__ inline unsigned row_scales(const Mx4Product& p, __amdgpu_buffer_rsrc_t s, int source, int kb)
+{
+    if (source == -2) return 0xffffu;
+    const unsigned at = source < 0 ? kPast : (unsigned)(source * p.lds) + kb;
+    const unsigned a = __builtin_amdgcn_raw_buffer_load_b8(s, kb < p.blocks ? at : kPast, 0, 0);
+    const unsigned b = __builtin_amdgcn_raw_buffer_load_b8(s, kb + 1 < p.blocks ? at + 1 : kPast, 0, 0);
+    return (kb < p.blocks ? a : 127u) | (kb + 1 < p.blocks ? b : 127u) << 8;
+}
+
+// What a lane needs of the channels it holds over NB blocks (from block b0 on) of one row group: one run of adjacent outputs, or two.
+template <bool GATED, int NB> struct Channels4 {
+    static constexpr int kRun = GATED ? 2 * NB : NB < 2 ? 4 * NB : 8, kRuns = (GATED ? 2 : 4) * NB / kRun;
+    int c0;   // first output of the first run; the second is 32 further on
+    f32x4 bias[NB];
+
+    __device__ inline void load(const Mx4Product& p, int expert, int group, int b0, int lane)
+    {
+        const int g = lane >> 4, half = p.channels / 2;
+        c0 = GATED ? group * 32 + g * 8 + b0 * 2 : group * 64 + (b0 >> 1) * 32 + g * 8 + (b0 & 1) * 4;
+        const float* from = p.bias ? p.bias + (int64_t)expert * p.channels : nullptr;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            bias[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (from) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if constexpr (GATED) {
+                        const int o = c0 + 2 * b + (r & 1);
+                        if (o < half) bias[b][r] = from[r < 2 ? o : half + o];
+                    } else {
+                        const int c = c0 + (b >> 1) * 32 + (b & 1) * 4 + r;
+                        if (c < p.channels) bias[b][r] = from[c];
+                    }
+                }
+            }
+        }
+    }
+};
+
+// The outputs of run `run` of a lane's sums for one row, in fp32.
+template <bool GATED, int NB>
+__device__ inline void outputs4(const Channels4<GATED, NB>& ch, const f32x4 (&acc)[NB], int run, float (&y)[Channels4<GATED, NB>::kRun])
+{
+    constexpr int PER = NB / Channels4<GATED, NB>::kRuns;   // blocks of a run
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int b = run * PER + i;
+        const f32x4 z = acc[b] + ch.bias[b];
+        if constexpr (GATED) {
+            y[2 * i] = silu_times(z[0], z[2]);
+            y[2 * i + 1] = silu_times(z[1], z[3]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[4 * i + r] = z[r];
+        }
+    }
+}
+
+// The largest over the lanes l, l ^ 16, l ^ 32, l ^ 48 (all four active): a block of 32 outputs of one row.
+__device__ inline unsigned column_max(unsigned m)
+{
+    m = max(m, (unsigned)__shfl_xor((int)m, 16));
+    return max(m, (unsigned)__shfl_xor((int)m, 32));
+}
+
+// Eight adjacent outputs of a lane, whose block of 32 the lanes l ^ 16, l ^ 32 and l ^ 48 share, as codes and the block's scale.  (Outputs
+// past the last channel are zeros.)
+__device__ inline unsigned rounded8(const float (&y)[8], unsigned& scale)
+{
+    unsigned most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, magnitude(y[e]));
+    scale = mx4_scale(column_max(most));
+    return mx4_codes(y, scale);
+}
+
+// Stores a lane's outputs of one row straight from the registers.  All lanes of a wavefront come here, also for rows that are not stored.
+template <bool GATED, int NB>
+__device__ inline void emit4(const Mx4Product& p, const Channels4<GATED, NB>& ch, const f32x4 (&acc)[NB], int64_t row, bool there)
+{
+    using C = Channels4<GATED, NB>;
+    constexpr int N = C::kRun;
+#pragma unroll
+    for (int run = 0; run < C::kRuns; ++run) {
+        const int c0 = ch.c0 + run * 32;
+        float y[N];
+        outputs4<GATED, NB>(ch, acc, run, y);
+        if constexpr (N == 8) {
+            if (p.out == NM_MX4) {
+                unsigned scale;
+                const unsigned codes = rounded8(y, scale);
+                const int block = c0 >> 5;
+                if (there && block * 32 < p.outs) {
+                    *reinterpret_cast<unsigned*>((uint8_t*)p.y + row * p.ldy + (size_t)(c0 >> 3) * 4) = codes;
+                    if ((c0 & 31) == 0) p.ys[row * p.ldys + block] = (uint8_t)scale;
+                }
+                continue;
+            }
+        }
+        if (!there) continue;
+        auto store = [&](auto bf16) {
+            constexpr bool BF16 = decltype(bf16)::value;
+            constexpr int ES = Elem<BF16>::kBytes;
+            char* py = (char*)p.y + row * p.ldy * ES;
+            const char* pr = !GATED && p.res ? (const char*)p.res + row * p.ldr * ES : nullptr;
+            if constexpr (N == 8) {
+                if (c0 + 8 <= p.outs) {
+                    if (pr) {
+                        float r[8];
+                        Elem<BF16>::load8(pr + (int64_t)c0 * ES, r);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] += r[e];
+                    }
+                    Elem<BF16>::store8(py + (int64_t)c0 * ES, y);
+                    return;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (c0 + i < p.outs) {
+                    if (pr) y[i] += Elem<BF16>::load1(pr + (int64_t)(c0 + i) * ES);
+                    Elem<BF16>::store1(py + (int64_t)(c0 + i) * ES, y[i]);
+                }
+            }
+        };
+        if (p.out == NM_BF16) store(std::true_type{});
+        else store(std::false_type{});
+    }
+}
+
+}  // namespace nm

@@ -1,7 +1,7 @@
-"""The feed-forward half of a transformer layer in 8-bit integers, through the C ABI:
+"""The feed-forward half of a transformer layer in 8-bit integers or in MX4, and with experts, through the C ABI:
 
     stream = x + residual
-    y = stream + down( round8( silu(gate) * up ) )      gate, up = products of round8( rmsnorm(stream) )
+    y = stream + down( round( silu(gate) * up ) )       gate, up = products of round( rmsnorm(stream) )
 
 This file only allocates tensors and sequences calls; all arithmetic is in the library's kernels.
 """
@@ -35,3 +35,64 @@ class FeedForwardQ8:
         return nm.nm_linear_q8(q, s, self.down, residual=x if h is None else h, dtype=x.dtype, stream=stream)
 
     __call__ = forward
+
+
+class FeedForwardMX4:
+    """gamma: fp32 [width]; up: gated weights (2 * hidden channels of `width`); down: `width` channels of `hidden`.
+    Weights packed by nm_mx4_pack; from_float() makes all three from fp32 or bf16 tensors."""
+
+    def __init__(self, gamma, up: nm.MX4Weights, down: nm.MX4Weights, eps: float = 1e-6):
+        _check_pair(up, down)
+        if up.experts != 1:
+            raise ValueError("up and down must be the weights of one expert")
+        self.gamma, self.up, self.down, self.eps = gamma, up, down, eps
+
+    @classmethod
+    def from_float(cls, gamma, gate_w, up_w, down_w, eps: float = 1e-6):
+        """gate_w, up_w [hidden, width], down_w [width, hidden] on the device, fp32 or bf16."""
+        import torch
+        return cls(gamma, nm.nm_mx4_pack(torch.cat([gate_w, up_w]), gated=True), nm.nm_mx4_pack(down_w), eps)
+
+    def forward(self, x, residual=None, stream=None):
+        """x, residual: [..., width] in bf16 or fp32.  Returns the new residual stream, shaped and typed like x."""
+        q, s, h = nm.nm_rmsnorm_mx4(x, self.gamma, residual, self.eps, stream=stream)
+        q, s = nm.nm_linear_mx4(q, s, self.up, rounded=True, stream=stream)
+        return nm.nm_linear_mx4(q, s, self.down, residual=x if h is None else h, dtype=x.dtype, stream=stream)
+
+    __call__ = forward
+
+
+class ExpertsMX4:
+    """A layer of experts: up: gated weights of each (2 * hidden channels of `width`), down: `width` channels of `hidden`;
+    every token goes through the k experts with its largest logits, whose answers are weighted with their softmax.
+    from_float() makes the weights from fp32 or bf16 tensors."""
+
+    def __init__(self, up: nm.MX4Weights, down: nm.MX4Weights, k: int, normalise: bool = True):
+        _check_pair(up, down)
+        if up.experts != down.experts or not 1 <= k <= up.experts:
+            raise ValueError(f"up has {up.experts} experts, down {down.experts}; {k} are chosen")
+        self.up, self.down, self.k, self.normalise = up, down, k, normalise
+
+    @classmethod
+    def from_float(cls, gate_w, up_w, down_w, k: int, normalise: bool = True):
+        """gate_w, up_w [experts, hidden, width], down_w [experts, width, hidden] on the device, fp32 or bf16."""
+        import torch
+        return cls(nm.nm_mx4_pack(torch.cat([gate_w, up_w], dim=1), gated=True), nm.nm_mx4_pack(down_w), k, normalise)
+
+    def forward(self, x, logits, residual=None, stream=None):
+        """x, residual: [..., width] in bf16 or fp32 (x: the normalised rows); logits [..., experts].  Returns residual plus the
+        experts' answers, shaped and typed like x.  The answers that are summed are bf16 for bf16 rows, fp32 for fp32."""
+        to = nm.nm_route(logits, self.k, self.normalise, stream=stream)
+        q, s = nm.nm_quantize_mx4(x, stream=stream)
+        q, s = nm.nm_experts_mx4(q, s, self.up, to.offsets, to.rows, rounded=True, stream=stream)
+        y = nm.nm_experts_mx4(q, s, self.down, to.offsets, dtype=x.dtype, stream=stream)
+        return nm.nm_combine(y, to.slots, to.weights, residual, dtype=x.dtype, stream=stream)
+
+    __call__ = forward
+
+
+def _check_pair(up, down):
+    if not up.gated or down.gated:
+        raise ValueError("up must be packed gated, down plain")
+    if up.outs != down.width or down.channels != up.width:
+        raise ValueError(f"up {up.channels} x {up.width} and down {down.channels} x {down.width} do not fit together")
