@@ -212,7 +212,8 @@ int product_call(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t l
     p.sources = (int)sources;
     p.out = dt;
     p.past = sy.rows * sy.width * (int64_t)es > ((int64_t)160 << 20);
-    const size_t need = mx4_workspace(p);
+    const Mx4Plan plan = mx4_plan(p);
+    const size_t need = plan.bytes();
     if (need) {
         if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16) {
             set_error("this call needs %zu bytes of workspace, 16-byte aligned; %zu were given", need,
@@ -224,7 +225,7 @@ int product_call(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t l
         NM_TRY(check_apart("workspace", sw, "y", sy, false));
         NM_TRY(check_apart("workspace", sw, "y_scales", sys, false));
     }
-    return run_mx4_product(p, workspace, (hipStream_t)stream);
+    return run_mx4_product(p, plan, workspace, (hipStream_t)stream);
 }
 
 // The integers of a block are 64 bits wide; one that does not fit an int is out of range for every argument that is one.
@@ -371,7 +372,7 @@ int nm_mx4_workspace(int64_t rows, const nm_mx4_t* w, int grouped, size_t* bytes
 {
     if (!w || !bytes) return null_block();
     NM_TRY(check_rows(rows, w->width));
-    *bytes = rows ? mx4_workspace(shape_of(w, rows, grouped != 0)) : 0;
+    *bytes = rows ? mx4_plan(shape_of(w, rows, grouped != 0)).bytes() : 0;
     return NM_OK;
 }
 

@@ -9,7 +9,7 @@
 // 2 (l / 16) and 2 (l / 16) + 1: their scales are adjacent bytes of a row in memory.
 //   d_w [experts][groups][steps][2 halves][4 blocks of rows][64 lanes][16 bytes]
 //       lane l of row block b holds packed row 16 b + l % 16, block of k 8 step + 2 (l / 16) + half
-//   d_s [experts][groups][steps][2 pairs][64 lanes] words of four scales: byte 2 (b & 1) + half of pair b / 2
+//   d_s [experts][groups][steps][2 halves][64 lanes] words of four scales, byte b that of row block b
 // Rows and blocks past the ends are zeros with the scale 1: whatever numbers meet them add nothing.
 struct nm_mx4 {
     int device = -1;
@@ -54,8 +54,16 @@ struct Mx4Product {
     nm_dtype_t out;       // NM_F32, NM_BF16 or NM_MX4
     int past;             // y is stored past the last-level cache
 };
-size_t mx4_workspace(const Mx4Product& p);
-int run_mx4_product(const Mx4Product& p, void* workspace, hipStream_t s);
+// What runs a call: a tile shape, or the few-row kernels (-1); and the workspace: what the tiles are, and the rows' scales as the tile
+// kernels read them.
+struct Mx4Plan {
+    int shape = -1;
+    int64_t tiles = 0;   // of rows, at most
+    size_t tile_bytes = 0, scale_bytes = 0;
+    size_t bytes() const { return tile_bytes + scale_bytes; }
+};
+Mx4Plan mx4_plan(const Mx4Product& p);
+int run_mx4_product(const Mx4Product& p, const Mx4Plan& plan, void* workspace, hipStream_t s);
 
 // routing (nm_experts.hip)
 struct Route {

@@ -12,6 +12,11 @@
 namespace nm {
 namespace {
 
+// The block of a step at place i of a row in LDS: those of the first half before those of the second.  (In the blocks' own order the four
+// blocks that an instruction takes of a row are every other one, and of what an LDS cycle reads two lie in the same banks: 12 % of a large
+// product's cycles.)
+__device__ inline int block_at(int i) { return 2 * (i & 3) + (i >> 2); }
+
 // ---------------------------------------------------------------- few rows
 // Tiles of up to 16 * TB rows.  A workgroup owns RB blocks of 16 packed channels; its NW wavefronts take the steps of 256 k in turn, U of them
 // in flight each, and add their sums through LDS at the end, in the order of the wavefronts.  Weights go from memory into registers: a
@@ -35,12 +40,12 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
     const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + group * p.steps * 8192, (unsigned)p.steps * 8192);
     const __amdgpu_buffer_rsrc_t ssr = q8_rsrc(p.ws + group * p.steps * 128, (unsigned)p.steps * 512);
     const RowBuffers from(p, t);
-    const unsigned woff = (b0 & 3) * 1024 + lane * 16, soff = ((b0 >> 1) & 1) * 256 + lane * 4;
+    const unsigned woff = (b0 & 3) * 1024 + lane * 16, soff = lane * 4;
     const unsigned mine = wave * (U * TB * 2048), lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem + mine;
     const unsigned at = mine + (lane & 15) * 128;
-    unsigned qoff[TB][2];   // 8 rows an instruction, block c of a row at c ^ (row & 7)
+    unsigned qoff[TB][2];   // 8 rows an instruction, place i of a row at i ^ (row & 7)
     int source[TB];
-    const int chunk = (lane & 7) ^ (lane >> 3);
+    const int chunk = block_at((lane & 7) ^ (lane >> 3));
 #pragma unroll
     for (int i = 0; i < TB; ++i) {
 #pragma unroll
@@ -53,7 +58,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
     f32x4 acc[RB][TB] = {};
     for (int k0 = wave; k0 < p.steps; k0 += NW * U) {
         i32x4 wf[U][2][RB];
-        unsigned wsc[U][RB == 4 ? 2 : 1], xsc[U][TB];
+        unsigned wsc[U][2], xsc[U][TB];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int k = k0 + u * NW;
@@ -71,27 +76,27 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
                     wf[u][h][i] = __builtin_bit_cast(
                         i32x4, __builtin_amdgcn_raw_buffer_load_b128(wsr, in ? woff + i * 1024 + (k * 2 + h) * 4096 : kPast, 0, 2));
 #pragma unroll
-            for (int i = 0; i < (RB == 4 ? 2 : 1); ++i) wsc[u][i] = __builtin_amdgcn_raw_buffer_load_b32(ssr, in ? soff + i * 256 + k * 512 : kPast, 0, 0);
+            for (int h = 0; h < 2; ++h) wsc[u][h] = __builtin_amdgcn_raw_buffer_load_b32(ssr, in ? soff + (k * 2 + h) * 256 : kPast, 0, 0);
 #pragma unroll
             for (int i = 0; i < TB; ++i) xsc[u][i] = row_scales(p, from.s, source[i], k * 8 + 2 * (lane >> 4));
         }
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if constexpr (RB == 1) wsc[u][0] >>= 16 * (b0 & 1);
             auto half = [&](auto hh) {
                 constexpr int h = decltype(hh)::value;
                 i32x4 xf[TB];
 #pragma unroll
                 for (int j = 0; j < TB; ++j)
-                    xf[j] = *reinterpret_cast<const i32x4*>(smem + at + u * TB * 2048 + j * 2048 + (((2 * (lane >> 4) + h) ^ (lane & 7)) << 4));
+                    xf[j] = *reinterpret_cast<const i32x4*>(smem + at + u * TB * 2048 + j * 2048 + (((4 * h + (lane >> 4)) ^ (lane & 7)) << 4));
+                const unsigned ws = RB == 4 ? wsc[u][h] : wsc[u][h] >> (8 * (b0 & 3));
 #pragma unroll
                 for (int j = 0; j < TB; ++j) {
-                    acc[0][j] = mma4<h, h>(wf[u][h][0], xf[j], acc[0][j], wsc[u][0], xsc[u][j]);
-                    if constexpr (RB >= 2) acc[1][j] = mma4<2 + h, h>(wf[u][h][1], xf[j], acc[1][j], wsc[u][0], xsc[u][j]);
+                    acc[0][j] = mma4<0, h>(wf[u][h][0], xf[j], acc[0][j], ws, xsc[u][j]);
+                    if constexpr (RB >= 2) acc[1][j] = mma4<1, h>(wf[u][h][1], xf[j], acc[1][j], ws, xsc[u][j]);
                     if constexpr (RB == 4) {
-                        acc[2][j] = mma4<h, h>(wf[u][h][2], xf[j], acc[2][j], wsc[u][1], xsc[u][j]);
-                        acc[3][j] = mma4<2 + h, h>(wf[u][h][3], xf[j], acc[3][j], wsc[u][1], xsc[u][j]);
+                        acc[2][j] = mma4<2, h>(wf[u][h][2], xf[j], acc[2][j], ws, xsc[u][j]);
+                        acc[3][j] = mma4<3, h>(wf[u][h][3], xf[j], acc[3][j], ws, xsc[u][j]);
                     }
                 }
             };
@@ -140,6 +145,309 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
     }
 }
 
+// ---------------------------------------------------------------- many rows
+// A workgroup of WR x WT wavefronts owns 64 * WR packed channels x 16 * TB * WT rows; a wavefront 64 x 16 TB of them.  K goes by in
+// steps of 256.  LDS holds NSW steps' weights and NSX steps' rows and scales, loaded straight into it: while a step is multiplied, the next one's
+// lie there and later ones' are on their way.  Operands are read from LDS half a step ahead, into the other half of the operand
+// registers, so one barrier a step is enough.
+// Weights lie in LDS as in memory (a wavefront's operand is 1 KiB of adjacent bytes); a row's 128 bytes are 8 blocks of 16 in the order of
+// block_at, place i stored at i ^ (row & 7), so that what an LDS cycle reads lies in different banks.
+template <int WR, int WT, int TB, int NSW, int NSX> struct Tile4 {
+    static constexpr int kWaves = WR * WT, kRows = 16 * TB * WT;
+    static constexpr int kWBytes = WR * 8192, kXBytes = kRows * 128, kSBytes = WR * 512 + kRows * 8;   // of a step
+    static constexpr int kWLoads = kWBytes / 1024 / kWaves, kXLoads = kXBytes / 1024 / kWaves;         // of 1 KiB, a wavefront and step
+    static constexpr int kSUnits = kSBytes / 256, kSLoads = (kSUnits + kWaves - 1) / kWaves;           // of 256 bytes: the first load the weights'
+    static constexpr int kSPitch = kSLoads * kWaves * 256;   // (units past the scales are loaded with nothing)
+    static_assert(WT == 2, "a load of scales is of weights' or of rows' in all wavefronts");
+    static constexpr int kXAt = NSW * kWBytes, kSAt = kXAt + NSX * kXBytes, kLds = kSAt + NSX * kSPitch;
+    static_assert(TB % 4 == 0 && kWBytes % (1024 * kWaves) == 0 && kXBytes % (1024 * kWaves) == 0, "every wavefront issues the same loads");
+    static_assert(kLds <= 160 * 1024 && NSW >= NSX && NSX >= 2, "");
+    // Loads that may be out while a step waits for the stages of the next: those of later steps.  Rows are loaded first, so with more stages
+    // of weights the weights of the step that goes with the last rows may be out too.
+    static constexpr int kLoads = kWLoads + kXLoads + kSLoads;
+    static constexpr int kOut = (NSX - 2) * kLoads + (NSW > NSX ? kWLoads : 0);
+};
+
+// The rows' scales of a tile and step as the kernel's lanes read them: [2 halves][rows / 64][64 lanes] words, byte j that of row block
+// 4 (rows / 64) + j.
+struct TileHead {
+    int tiles, pad[3];
+};
+struct TileRows {
+    int expert, count;
+    int64_t row0;
+};
+
+__global__ __launch_bounds__(256) void mx4_scales_kernel(Mx4Product p, int per, int parts, TileHead* head, TileRows* tiles, unsigned* to)
+{
+    const int tile = blockIdx.x / parts, part = blockIdx.x - tile * parts;
+    const RowTile t = row_tile(p, tile, per);
+    if (part == 0 && threadIdx.x == 0) {
+        tiles[tile] = {t.expert, t.count, t.row0};
+        if (p.grouped && t.count > 0) atomicMax(&head->tiles, tile + 1);
+    }
+    if (t.count == 0) return;
+    const int first = part * 256 + threadIdx.x, words = p.steps * per * 2;
+    if (first >= words) return;
+    const int lane = first & 63, j4 = (first >> 6) % (per / 64), half = (first >> 6) / (per / 64) & 1, step = (first >> 6) / (per / 64) >> 1;
+    const int kb = step * 8 + 2 * (lane >> 4) + half;
+    const int64_t base = p.index ? 0 : t.row0;
+    unsigned word = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int src = source_of(p, t, (j4 * 4 + j) * 16 + (lane & 15));
+        unsigned s = 127;   // past the row's blocks codes of 0 are multiplied
+        if (src == -2) s = 255;
+        else if (src >= 0 && kb < p.blocks) s = p.s[(base + src) * p.lds + kb];
+        word |= s << (8 * j);
+    }
+    to[(int64_t)tile * words + first] = word;
+}
+
+__global__ void mx4_head_kernel(TileHead* head) { head->tiles = 0; }
+
+// 4 bytes a lane from memory to LDS at `lds` + 4 * lane, as load_to_lds.
+__device__ inline void load_to_lds4(__amdgpu_buffer_rsrc_t r, unsigned voff, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : :
+                 "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(r));
+}
+
+constexpr int largest_divisor4(int n, int most) { return most >= n ? n : n % most == 0 ? most : largest_divisor4(n, most - 1); }
+
+// A workgroup's outputs through LDS, so that whole rows of its tile are stored, 16 bytes a thread and adjacent threads adjacent.  JP of
+// the TB blocks of rows at a time, STAGE32 in fp32 (fp32 outputs, and for a residual, so that it rounds once), or as what is stored.  The
+// 16-byte pieces of a row lie at piece ^ (row & 7) (fewer bits for rows of fewer pieces).
+template <int WR, int WT, int TB, int JP, bool STAGE32, bool GATED, int OUT>
+__device__ inline void store_tile4(const Mx4Product& p, const Channels4<GATED, 4>& ch, const f32x4 (&acc)[TB][4], char* smem,
+                                   int wr, int wt, int lane, int group0, const TileRows& t)
+{
+    constexpr bool MX = OUT == NM_MX4, BF16 = OUT == NM_BF16;
+    constexpr int C = Channels4<GATED, 4>::kRuns * 8;   // outputs of a group and lane
+    constexpr int kOuts = WR * C * 4, kThreads = WR * WT * 64, kRows = WT * JP * 16;
+    constexpr int kPitch = MX ? kOuts / 2 : kOuts * (STAGE32 ? 4 : 2), kHas = kPitch / 16, kMask = kHas >= 8 ? 7 : kHas - 1;
+    constexpr int kPieces = MX ? kHas : kOuts * (BF16 ? 2 : 4) / 16, kPer = kOuts / kPieces;   // 16-byte pieces of a stored row; values in one
+    constexpr int ES = BF16 ? 2 : 4;
+    const int col0 = group0 * C * 4;
+    const bool past = p.past;
+#pragma unroll
+    for (int j0 = 0; j0 < TB; j0 += JP) {
+        __syncthreads();   // the stages, or the outputs before, have been read
+#pragma unroll
+        for (int jj = 0; jj < JP; ++jj) {
+            const int lrow = (wt * JP + jj) * 16 + (lane & 15);
+            char* to = smem + lrow * kPitch;
+#pragma unroll
+            for (int run = 0; run < Channels4<GATED, 4>::kRuns; ++run) {
+                float y[8];
+                outputs4<GATED, 4>(ch, acc[j0 + jj], run, y);
+                const int c = wr * C * 4 + run * 32 + (lane >> 4) * 8;   // column in the tile
+                if constexpr (MX) {
+                    unsigned scale;
+                    const unsigned codes = rounded8(y, scale);
+                    *reinterpret_cast<unsigned*>(to + ((c >> 5) ^ (lrow & kMask)) * 16 + (lane >> 4) * 4) = codes;
+                    const int row = (wt * TB + j0 + jj) * 16 + (lane & 15), block = (col0 + c) >> 5;
+                    if ((lane >> 4) == 0 && row < t.count && block * 32 < p.outs) p.ys[(t.row0 + row) * p.ldys + block] = (uint8_t)scale;
+                } else if constexpr (STAGE32) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        *reinterpret_cast<f32x4*>(to + (((c >> 2) + h) ^ (lrow & 7)) * 16) = f32x4{y[4 * h], y[4 * h + 1], y[4 * h + 2], y[4 * h + 3]};
+                } else {
+                    u32x4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = bf16_pair(y[2 * i], y[2 * i + 1]);
+                    *reinterpret_cast<u32x4*>(to + ((c >> 3) ^ (lrow & 7)) * 16) = v;
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int u = threadIdx.x; u < kRows * kPieces; u += kThreads) {
+            const int lrow = u / kPieces, piece = u % kPieces;
+            const int trow = (lrow / (JP * 16)) * TB * 16 + j0 * 16 + lrow % (JP * 16), col = col0 + piece * kPer;
+            if (trow >= t.count || col >= p.outs) continue;
+            const int64_t row = t.row0 + trow;
+            const char* from = smem + lrow * kPitch;
+            if constexpr (MX) {
+                store16((char*)p.y + row * p.ldy + (size_t)(col >> 5) * 16, *reinterpret_cast<const u32x4*>(from + (piece ^ (lrow & kMask)) * 16), past);
+            } else {
+                char* py = (char*)p.y + (row * p.ldy + col) * ES;
+                u32x4 v;
+                if constexpr (STAGE32 && BF16) {
+                    const f32x4 a = *reinterpret_cast<const f32x4*>(from + ((2 * piece) ^ (lrow & 7)) * 16);
+                    const f32x4 b = *reinterpret_cast<const f32x4*>(from + ((2 * piece + 1) ^ (lrow & 7)) * 16);
+                    float y[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+                    if (p.res) {
+                        const char* pr = (const char*)p.res + (row * p.ldr + col) * ES;
+                        if (col + 8 <= p.outs) {
+                            float r[8];
+                            Elem<true>::load8(pr, r);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) y[e] += r[e];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (col + e < p.outs) y[e] += Elem<true>::load1(pr + e * 2);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = bf16_pair(y[2 * i], y[2 * i + 1]);
+                } else {
+                    v = *reinterpret_cast<const u32x4*>(from + (piece ^ (lrow & 7)) * 16);
+                    if (!BF16 && p.res) {
+                        const char* pr = (const char*)p.res + (row * p.ldr + col) * 4;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (col + e < p.outs) v[e] = __float_as_uint(__uint_as_float(v[e]) + Elem<false>::load1(pr + e * 4));
+                    }
+                }
+                if (col + kPer <= p.outs) {
+                    store16(py, v, past);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e)
+                        if (col + e < p.outs) {
+                            if constexpr (BF16) { const unsigned short h = (unsigned short)(v[e / 2] >> (16 * (e & 1))); __builtin_memcpy(py + e * 2, &h, 2); }
+                            else { const unsigned w = v[e]; __builtin_memcpy(py + e * 4, &w, 4); }
+                        }
+                }
+            }
+        }
+    }
+}
+
+template <int WR, int WT, int TB, int NSW, int NSX, bool GATED, int OUT>
+__global__ __launch_bounds__(WR * WT * 64) void mx4_tile_kernel(Mx4Product p, TileOrder order, const TileHead* head, const TileRows* tiles,
+                                                               const unsigned* scales)
+{
+    using T = Tile4<WR, WT, TB, NSW, NSX>;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wr = wave % WR, wt = wave / WR;
+    int tc, tr, tile, split;
+    if (p.grouped) {   // (tiles past those that there are end here, so that the others are dealt to all XCDs)
+        order.tiles_r = head->tiles;
+        if ((int)blockIdx.x >= order.tiles()) return;
+    }
+    order.at(blockIdx.x, tc, tr, tile, split);
+    const TileRows t = tiles[tr];
+    const int g0 = tc * WR;
+    const int ngrp = p.groups - g0 < WR ? p.groups - g0 : WR;
+    const int steps = p.steps;
+    const size_t group0 = (size_t)t.expert * p.groups + g0;
+    const RowTile rt{t.expert, t.count, t.row0};
+    const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + group0 * steps * 8192, (unsigned)ngrp * steps * 8192);
+    const __amdgpu_buffer_rsrc_t gsr = q8_rsrc(p.ws + group0 * steps * 128, (unsigned)ngrp * steps * 512);
+    const __amdgpu_buffer_rsrc_t xsr = RowBuffers(p, rt).q;
+    const __amdgpu_buffer_rsrc_t ssr = q8_rsrc(scales + (size_t)tr * steps * T::kRows * 2, (unsigned)steps * T::kRows * 8);
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem;
+    // Rows past the tile's last read its first: what comes of them is not stored.  (The scale of a row for an index outside x is NaN.)
+    unsigned xvoff[T::kXLoads];
+    const int chunk = block_at((lane & 7) ^ (lane >> 3));   // the block of a step that the lane loads (row & 7 is lane >> 3)
+#pragma unroll
+    for (int i = 0; i < T::kXLoads; ++i) {
+        const int row = (wave + i * T::kWaves) * 8 + (lane >> 3), src = source_of(p, rt, row);
+        xvoff[i] = (unsigned)((src < 0 ? 0 : src) * p.ldq) + chunk * 16;
+    }
+    const int xsteps = (p.blocks + 7 - chunk) >> 3;         // steps that have it
+    const unsigned lane16 = lane * 16, lane4 = lane * 4;
+    // load i of a step: rows and scales of step sx, weights of step sw; past the last step nothing is read, so that the count of loads holds
+    auto fetch = [&](int i, int sw, unsigned wat, int sx, unsigned xat, unsigned sat) {
+        constexpr unsigned kNone = 0xc0000000u;   // (and what a lane adds: past the end of weights and scales)
+        if (i < T::kXLoads) {
+            load_to_lds(xsr, sx < xsteps ? xvoff[i] + (unsigned)sx * 128 : kPast, lds0 + T::kXAt + xat + (wave + i * T::kWaves) * 1024);
+        } else if (i == T::kXLoads) {
+            load_to_lds4(gsr, (sx < steps ? ((unsigned)((wave >> 1) * steps + sx) * 2 + (wave & 1)) * 256 : kNone) + lane4, lds0 + T::kSAt + sat + wave * 256);
+        } else if (i < T::kXLoads + T::kSLoads) {
+            const int u = wave + (i - T::kXLoads - 1) * T::kWaves;
+            load_to_lds4(ssr, (sx < steps && u < T::kRows / 32 ? (unsigned)sx * (T::kRows * 8) + u * 256 : kNone) + lane4,
+                         lds0 + T::kSAt + sat + (wave + (i - T::kXLoads) * T::kWaves) * 256);
+        } else {
+            const int n = i - T::kXLoads - T::kSLoads, c = wave + n * T::kWaves;   // 1 KiB of the stage
+            load_to_lds(wsr, (sw < steps ? ((unsigned)(c >> 3) * steps + sw) * 8192 + (c & 7) * 1024 : kNone) + lane16, lds0 + wat + c * 1024);
+        }
+    };
+    const int wlane = wr * 8192 + lane * 16;
+    const int xlane = T::kXAt + (wt * TB * 16 + (lane & 15)) * 128;
+    const int slane = T::kSAt + lane * 4;
+    i32x4 f[2][4 + TB];               // operands of the two halves of a step: 4 blocks of weights, TB of rows
+    unsigned fs[2][1 + TB / 4];       // and their scales
+    constexpr int READS = 4 + TB + 1 + TB / 4;
+    auto read = [&](int h, int i, unsigned wat, unsigned xat, unsigned sat) {
+        if (i < 4) f[h][i] = *reinterpret_cast<const i32x4*>(smem + wat + wlane + h * 4096 + i * 1024);
+        else if (i < 4 + TB) f[h][i] = *reinterpret_cast<const i32x4*>(smem + xat + xlane + (((4 * h + (lane >> 4)) ^ (lane & 7)) << 4) + (i - 4) * 2048);
+        else if (i == 4 + TB) fs[h][0] = *reinterpret_cast<const unsigned*>(smem + sat + slane + wr * 512 + h * 256);
+        else fs[h][i - 4 - TB] = *reinterpret_cast<const unsigned*>(smem + sat + slane + WR * 512 + h * (T::kRows * 4) + (wt * (TB / 4) + i - 5 - TB) * 256);
+    };
+    f32x4 acc[TB][4] = {};
+    constexpr int LOADS = T::kLoads;
+#pragma unroll
+    for (int s = 0; s < NSX; ++s)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) fetch(i, s, s * T::kWBytes, s, s * T::kXBytes, s * T::kSPitch);
+#pragma unroll
+    for (int s = NSX; s < NSW; ++s)
+#pragma unroll
+        for (int i = T::kXLoads + T::kSLoads; i < LOADS; ++i) fetch(i, s, s * T::kWBytes, 0, 0, 0);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((NSX - 1) * LOADS + (NSW - NSX) * T::kWLoads) : "memory");
+#pragma unroll
+    for (int i = 0; i < READS; ++i) read(0, i, 0, 0, 0);
+    auto multiply = [&](int h, int j) {
+        const unsigned ws = fs[h][0], xs = fs[h][1 + j / 4];
+        auto four = [&](auto ox) {
+            constexpr int OX = decltype(ox)::value;
+            acc[j][0] = mma4<0, OX>(f[h][0], f[h][4 + j], acc[j][0], ws, xs);
+            acc[j][1] = mma4<1, OX>(f[h][1], f[h][4 + j], acc[j][1], ws, xs);
+            acc[j][2] = mma4<2, OX>(f[h][2], f[h][4 + j], acc[j][2], ws, xs);
+            acc[j][3] = mma4<3, OX>(f[h][3], f[h][4 + j], acc[j][3], ws, xs);
+        };
+        if (j % 4 == 0) four(std::integral_constant<int, 0>{});
+        else if (j % 4 == 1) four(std::integral_constant<int, 1>{});
+        else if (j % 4 == 2) four(std::integral_constant<int, 2>{});
+        else four(std::integral_constant<int, 3>{});
+    };
+    unsigned wnow = 0, xnow = 0, snow = 0;   // the stages that are multiplied
+    for (int k = 0; k < steps; ++k) {
+        const unsigned wnext = wnow + T::kWBytes == NSW * T::kWBytes ? 0 : wnow + T::kWBytes;
+        const unsigned xnext = xnow + T::kXBytes == NSX * T::kXBytes ? 0 : xnow + T::kXBytes;
+        const unsigned snext = snow + T::kSPitch == NSX * T::kSPitch ? 0 : snow + T::kSPitch;
+        // first half: its operands are in registers; the second half's are read meanwhile
+#pragma unroll
+        for (int j = 0; j < TB; ++j) {
+#pragma unroll
+            for (int i = j * READS / TB; i < (j + 1) * READS / TB; ++i) read(1, i, wnow, xnow, snow);
+            multiply(0, j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // these stages have been read, the next ones have landed
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(T::kOut) : "memory");
+        // second half: the next step's first operands are read, and what comes after the last stages in LDS is loaded in these ones' place
+#pragma unroll
+        for (int j = 0; j < TB; ++j) {
+#pragma unroll
+            for (int i = j * READS / TB; i < (j + 1) * READS / TB; ++i) read(0, i, wnext, xnext, snext);
+#pragma unroll
+            for (int i = j * LOADS / TB; i < (j + 1) * LOADS / TB; ++i)
+                fetch(i, k + NSW, wnow, k + NSX, xnow, snow);
+            multiply(1, j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        wnow = wnext;
+        xnow = xnext;
+        snow = snext;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // no load into LDS outlives the workgroup
+    Channels4<GATED, 4> ch;
+    ch.load(p, t.expert, g0 + wr < p.groups ? g0 + wr : p.groups - 1, 0, lane);   // (what a wavefront past the last group has is not stored)
+    constexpr int kOuts = WR * Channels4<GATED, 4>::kRuns * 32;
+    constexpr int JP4 = largest_divisor4(TB, T::kLds / (16 * WT * kOuts * 4)), JP2 = largest_divisor4(TB, T::kLds / (16 * WT * kOuts * 2)),
+                  JPM = largest_divisor4(TB, T::kLds / (16 * WT * kOuts / 2));
+    if constexpr (OUT == NM_MX4) store_tile4<WR, WT, TB, JPM, false, GATED, OUT>(p, ch, acc, smem, wr, wt, lane, g0, t);
+    else if constexpr (OUT == NM_F32) store_tile4<WR, WT, TB, JP4, true, GATED, OUT>(p, ch, acc, smem, wr, wt, lane, g0, t);
+    else if (p.res) store_tile4<WR, WT, TB, JP4, true, GATED, OUT>(p, ch, acc, smem, wr, wt, lane, g0, t);
+    else store_tile4<WR, WT, TB, JP2, false, GATED, OUT>(p, ch, acc, smem, wr, wt, lane, g0, t);
+}
+
 // ---------------------------------------------------------------- weights
 // Codes of block kb of a row without those past the width.
 __device__ inline i32x4 block_codes(const uint8_t* row, int kb, int width)
@@ -155,7 +463,7 @@ __device__ inline i32x4 block_codes(const uint8_t* row, int kb, int width)
     return v;
 }
 
-// One 16-byte unit of the packed weights a thread, and a word of scales for every 16 of them.
+// One 16-byte unit of the packed weights a thread; those of the first row block also the words of scales.
 __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t lds, uint8_t* to,
                                                        unsigned* to_scales, int experts, int channels, int width, int gated, int groups,
                                                        int steps, int blocks, int* bad)
@@ -170,17 +478,17 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* q, int64_t
         i32x4 v = {0, 0, 0, 0};
         if (c >= 0 && kb < blocks) v = block_codes(q + (expert * channels + c) * ldq, kb, width);
         *reinterpret_cast<i32x4*>(to + i * 16) = v;
-        if (h == 0 && (b & 1) == 0) {
+        if (b == 0) {
             unsigned word = 0;
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-                const int cn = q8_row_of(group * 64 + (b + (n >> 1)) * 16 + (lane & 15), channels, gated), kn = step * 8 + 2 * (lane >> 4) + (n & 1);
-                unsigned s = 127;
-                if (cn >= 0 && kn < blocks) s = scales[(expert * channels + cn) * lds + kn];
-                if (s == 255) atomicOr(bad, 1);
-                word |= s << (8 * n);
+                const int cn = q8_row_of(group * 64 + n * 16 + (lane & 15), channels, gated);
+                unsigned scale = 127;
+                if (cn >= 0 && kb < blocks) scale = scales[(expert * channels + cn) * lds + kb];
+                if (scale == 255) atomicOr(bad, 1);
+                word |= scale << (8 * n);
             }
-            to_scales[(gk * 2 + (b >> 1)) * 64 + lane] = word;
+            to_scales[(gk * 2 + h) * 64 + lane] = word;
         }
     }
 }
@@ -198,7 +506,7 @@ __global__ __launch_bounds__(256) void mx4_unpack_kernel(const uint8_t* from, co
         if (c < 0 || kb >= blocks) continue;
         const int64_t row = expert * channels + c;
         *reinterpret_cast<i32x4*>(q + (row * blocks + kb) * 16) = *reinterpret_cast<const i32x4*>(from + i * 16);
-        scales[row * blocks + kb] = (uint8_t)(from_scales[(gk * 2 + (b >> 1)) * 64 + lane] >> (8 * (2 * (b & 1) + h)));
+        scales[row * blocks + kb] = (uint8_t)(from_scales[(gk * 2 + h) * 64 + lane] >> (8 * b));
     }
 }
 
@@ -238,12 +546,82 @@ int pick_few4(const Mx4Product& p, hipStream_t s)
     return launch_few4<TB, 1, 8, U>(p, s);
 }
 
+// The tile kernels' shapes.
+struct Shape4 {
+    int wr, rows, waves;
+};
+constexpr Shape4 kShapes4[] = {{4, 256, 8},    // 256 packed channels x 256 rows
+                               {4, 128, 8},
+                               {2, 128, 4}};
+
+template <int SHAPE, int WT, int TB, int NSW, int NSX, bool GATED, int OUT>
+int launch_tile4(const Mx4Product& p, const Mx4Plan& pl, char* workspace, hipStream_t s)
+{
+    constexpr int WR = kShapes4[SHAPE].wr;
+    using T = Tile4<WR, WT, TB, NSW, NSX>;
+    static_assert(T::kWaves == kShapes4[SHAPE].waves && T::kRows == kShapes4[SHAPE].rows, "kShapes4 describes the kernels");
+    TileOrder o;
+    o.splits = 1;
+    o.tiles_c = (p.groups + WR - 1) / WR;
+    o.tiles_r = (int)pl.tiles;
+    const int64_t grid = pl.tiles * o.tiles_c;
+    const int parts = (p.steps * T::kRows * 2 + 255) / 256;
+    if (grid > 0x7fffffff || pl.tiles * parts > 0x7fffffff) {
+        set_error("%lld workgroups: too many", (long long)(grid > pl.tiles * parts ? grid : pl.tiles * parts));
+        return NM_ERR_SHAPE;
+    }
+    TileHead* head = (TileHead*)workspace;
+    TileRows* tiles = (TileRows*)(head + 1);
+    unsigned* scales = (unsigned*)(workspace + pl.tile_bytes);
+    if (p.grouped) {
+        hipLaunchKernelGGL(mx4_head_kernel, dim3(1), dim3(1), 0, s, head);
+        NM_HIP_CHECK(hipGetLastError());
+    }
+    hipLaunchKernelGGL(mx4_scales_kernel, dim3((unsigned)(pl.tiles * parts)), dim3(256), 0, s, p, T::kRows, parts, head, tiles, scales);
+    NM_HIP_CHECK(hipGetLastError());
+    static unsigned long long done = 0;
+    const int rc = allow_lds((const void*)mx4_tile_kernel<WR, WT, TB, NSW, NSX, GATED, OUT>, T::kLds, &done);
+    if (rc != NM_OK) return rc;
+    hipLaunchKernelGGL((mx4_tile_kernel<WR, WT, TB, NSW, NSX, GATED, OUT>), dim3((unsigned)grid), dim3(T::kWaves * 64), T::kLds, s, p, o,
+                       (const TileHead*)head, (const TileRows*)tiles, (const unsigned*)scales);
+    NM_HIP_CHECK(hipGetLastError());
+    return NM_OK;
+}
+
+template <bool GATED, int OUT>
+int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, char* workspace, hipStream_t s)
+{
+    switch (pl.shape) {
+    case 0: return launch_tile4<0, 2, 8, 2, 2, GATED, OUT>(p, pl, workspace, s);
+    case 1: return launch_tile4<1, 2, 4, 3, 3, GATED, OUT>(p, pl, workspace, s);
+    default: return launch_tile4<2, 2, 4, 2, 2, GATED, OUT>(p, pl, workspace, s);
+    }
+}
+
 }  // namespace
 
-size_t mx4_workspace(const Mx4Product&) { return 0; }
-
-int run_mx4_product(const Mx4Product& p, void*, hipStream_t s)
+Mx4Plan mx4_plan(const Mx4Product& p)
 {
+    Mx4Plan pl;
+    const int64_t each = p.grouped ? (p.rows + p.experts - 1) / p.experts : p.rows;
+    if (each <= NM_MX4_FEW_ROWS) return pl;
+    pl.shape = each >= 256 ? 0 : 2;
+    if (pl.shape < 0) return pl;
+    const int per = kShapes4[pl.shape].rows;
+    pl.tiles = tiles_of(p, per);
+    pl.tile_bytes = (sizeof(TileHead) + (size_t)pl.tiles * sizeof(TileRows) + 255) / 256 * 256;
+    pl.scale_bytes = (size_t)pl.tiles * p.steps * per * 8;
+    return pl;
+}
+
+int run_mx4_product(const Mx4Product& p, const Mx4Plan& pl, void* workspace, hipStream_t s)
+{
+    if (pl.shape >= 0) {
+        char* ws = (char*)workspace;
+        if (p.out == NM_MX4) return p.gated ? pick_tile4<true, NM_MX4>(p, pl, ws, s) : pick_tile4<false, NM_MX4>(p, pl, ws, s);
+        if (p.out == NM_BF16) return p.gated ? pick_tile4<true, NM_BF16>(p, pl, ws, s) : pick_tile4<false, NM_BF16>(p, pl, ws, s);
+        return p.gated ? pick_tile4<true, NM_F32>(p, pl, ws, s) : pick_tile4<false, NM_F32>(p, pl, ws, s);
+    }
     const int64_t each = p.grouped ? (p.rows + p.experts - 1) / p.experts : p.rows;
     if (each <= 16) return pick_few4<1>(p, s);
     if (each <= 32) return pick_few4<2>(p, s);
