@@ -5,10 +5,9 @@
 #include "nm_q8_internal.h"
 
 // Packed weights.  Channels are dealt to packed rows as in 8 bits (q8_row_of), 64 of them a row group.  A step is 256 k, 8 blocks; in a
-// 16x16x128 matrix instruction lane l holds one block of one row, and of the two instructions of a step ("halves") lane l takes blocks
-// 2 (l / 16) and 2 (l / 16) + 1: their scales are adjacent bytes of a row in memory.
+// 16x16x128 matrix instruction, half a step, lane l holds one block of one row.
 //   d_w [experts][groups][steps][2 halves][4 blocks of rows][64 lanes][16 bytes]
-//       lane l of row block b holds packed row 16 b + l % 16, block of k 8 step + 2 (l / 16) + half
+//       lane l of row block b holds packed row 16 b + l % 16, block of k 8 step + 4 half + l / 16
 //   d_s [experts][groups][steps][2 halves][64 lanes] words of four scales, byte b that of row block b
 // Rows and blocks past the ends are zeros with the scale 1: whatever numbers meet them add nothing.
 struct nm_mx4 {

@@ -23,14 +23,17 @@ struct RowTile {
 };
 
 // Tile number `tile` of `per` rows: the groups' tiles follow one another.  Every wavefront looks for itself, 64 groups at a time.
-// count is 0 past the last group's last tile.
-__device__ inline RowTile row_tile(const Mx4Product& p, int tile, int per)
+// count is 0 past the last group's last tile.  `to_end`: all groups are looked at, and *all gets the number of tiles that there are.
+__device__ inline RowTile row_tile(const Mx4Product& p, int tile, int per, bool to_end = false, int* all = nullptr)
 {
     if (!p.grouped) {
         const int64_t row0 = (int64_t)tile * per;
+        if (to_end) *all = (int)((p.rows + (int64_t)per - 1) / per);
         return {0, (int)(p.rows - row0 < per ? p.rows - row0 : per), row0};
     }
     const int lane = threadIdx.x & 63;
+    RowTile found{0, 0, 0};
+    int before = 0;
     for (int e0 = 0; e0 < p.experts; e0 += 64) {
         const int e = e0 + lane;
         int from = 0, n = 0;
@@ -44,16 +47,18 @@ __device__ inline RowTile row_tile(const Mx4Product& p, int tile, int per)
             const int up = __shfl_up(to, d);
             if (lane >= d) to += up;
         }
-        const unsigned long long past = __ballot(to > tile);
-        if (past) {
-            const int l = __ffsll(past) - 1;
-            const int in = __builtin_amdgcn_readfirstlane(tile - (__shfl(to, l) - __shfl(tiles, l)));
+        const int here = __builtin_amdgcn_readlane(to, 63);
+        if (found.count == 0 && tile < before + here) {
+            const int l = __ffsll(__ballot(before + to > tile)) - 1;
+            const int in = __builtin_amdgcn_readfirstlane(tile - before - (__shfl(to, l) - __shfl(tiles, l)));
             const int left = __builtin_amdgcn_readfirstlane(__shfl(n, l)) - in * per;
-            return {e0 + l, left < per ? left : per, (int64_t)__builtin_amdgcn_readfirstlane(__shfl(from, l)) + (int64_t)in * per};
+            found = {e0 + l, left < per ? left : per, (int64_t)__builtin_amdgcn_readfirstlane(__shfl(from, l)) + (int64_t)in * per};
+            if (!to_end) return found;
         }
-        tile -= __builtin_amdgcn_readlane(to, 63);
+        before += here;
     }
-    return {0, 0, 0};
+    if (to_end) *all = before;
+    return found;
 }
 
 // Where row `row` of a tile comes from: rows of x from `base` on that the kernels' buffers begin with.  -1: nowhere.
@@ -77,15 +82,15 @@ struct RowBuffers {
     }
 };
 
-// The two scales of a row that a lane needs in a step, as the low bytes of a word: blocks kb and kb + 1.  Past the row's blocks 1 (the
+// The two scales of a row that a lane needs in a step, as the low bytes of a word: blocks kb and kb + 4.  Past the row's blocks 1 (the
 // codes there meet zeros), for an index outside x NaN.
 __device__ inline unsigned row_scales(const Mx4Product& p, __amdgpu_buffer_rsrc_t s, int source, int kb)
 {
     if (source == -2) return 0xffffu;
     const unsigned at = source < 0 ? kPast : (unsigned)(source * p.lds) + kb;
     const unsigned a = __builtin_amdgcn_raw_buffer_load_b8(s, kb < p.blocks ? at : kPast, 0, 0);
-    const unsigned b = __builtin_amdgcn_raw_buffer_load_b8(s, kb + 1 < p.blocks ? at + 1 : kPast, 0, 0);
-    return (kb < p.blocks ? a : 127u) | (kb + 1 < p.blocks ? b : 127u) << 8;
+    const unsigned b = __builtin_amdgcn_raw_buffer_load_b8(s, kb + 4 < p.blocks ? at + 4 : kPast, 0, 0);
+    return (kb < p.blocks ? a : 127u) | (kb + 4 < p.blocks ? b : 127u) << 8;
 }
 
 // What a lane needs of the channels it holds over NB blocks (from block b0 on) of one row group: one run of adjacent outputs, or two.
@@ -118,6 +123,9 @@ template <bool GATED, int NB> struct Channels4 {
     }
 };
 
+// silu(gate) * up.  The reciprocal is within 1 u of 2 u = 2^-23, as the quotient of silu_times; that takes four times as many instructions.
+__device__ inline float silu4(float gate, float up) { return gate * __builtin_amdgcn_rcpf(1.0f + __expf(-gate)) * up; }
+
 // The outputs of run `run` of a lane's sums for one row, in fp32.
 template <bool GATED, int NB>
 __device__ inline void outputs4(const Channels4<GATED, NB>& ch, const f32x4 (&acc)[NB], int run, float (&y)[Channels4<GATED, NB>::kRun])
@@ -128,8 +136,8 @@ __device__ inline void outputs4(const Channels4<GATED, NB>& ch, const f32x4 (&ac
         const int b = run * PER + i;
         const f32x4 z = acc[b] + ch.bias[b];
         if constexpr (GATED) {
-            y[2 * i] = silu_times(z[0], z[2]);
-            y[2 * i + 1] = silu_times(z[1], z[3]);
+            y[2 * i] = silu4(z[0], z[2]);
+            y[2 * i + 1] = silu4(z[1], z[3]);
         } else {
 #pragma unroll
             for (int r = 0; r < 4; ++r) y[4 * i + r] = z[r];
@@ -140,8 +148,10 @@ __device__ inline void outputs4(const Channels4<GATED, NB>& ch, const f32x4 (&ac
 // The largest over the lanes l, l ^ 16, l ^ 32, l ^ 48 (all four active): a block of 32 outputs of one row.
 __device__ inline unsigned column_max(unsigned m)
 {
-    m = max(m, (unsigned)__shfl_xor((int)m, 16));
-    return max(m, (unsigned)__shfl_xor((int)m, 32));
+    const u32x2 a = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    m = max(a[0], a[1]);
+    const u32x2 b = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    return max(b[0], b[1]);
 }
 
 // Eight adjacent outputs of a lane, whose block of 32 the lanes l ^ 16, l ^ 32 and l ^ 48 share, as codes and the block's scale.  (Outputs

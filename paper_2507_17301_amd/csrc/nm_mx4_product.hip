@@ -12,11 +12,6 @@
 namespace nm {
 namespace {
 
-// The block of a step at place i of a row in LDS: those of the first half before those of the second.  (In the blocks' own order the four
-// blocks that an instruction takes of a row are every other one, and of what an LDS cycle reads two lie in the same banks: 12 % of a large
-// product's cycles.)
-__device__ inline int block_at(int i) { return 2 * (i & 3) + (i >> 2); }
-
 // ---------------------------------------------------------------- few rows
 // Tiles of up to 16 * TB rows.  A workgroup owns RB blocks of 16 packed channels; its NW wavefronts take the steps of 256 k in turn, U of them
 // in flight each, and add their sums through LDS at the end, in the order of the wavefronts.  Weights go from memory into registers: a
@@ -43,9 +38,9 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
     const unsigned woff = (b0 & 3) * 1024 + lane * 16, soff = lane * 4;
     const unsigned mine = wave * (U * TB * 2048), lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem + mine;
     const unsigned at = mine + (lane & 15) * 128;
-    unsigned qoff[TB][2];   // 8 rows an instruction, place i of a row at i ^ (row & 7)
+    unsigned qoff[TB][2];   // 8 rows an instruction, block c of a row at c ^ (row & 7)
     int source[TB];
-    const int chunk = block_at((lane & 7) ^ (lane >> 3));
+    const int chunk = (lane & 7) ^ (lane >> 3);
 #pragma unroll
     for (int i = 0; i < TB; ++i) {
 #pragma unroll
@@ -78,7 +73,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
 #pragma unroll
             for (int h = 0; h < 2; ++h) wsc[u][h] = __builtin_amdgcn_raw_buffer_load_b32(ssr, in ? soff + (k * 2 + h) * 256 : kPast, 0, 0);
 #pragma unroll
-            for (int i = 0; i < TB; ++i) xsc[u][i] = row_scales(p, from.s, source[i], k * 8 + 2 * (lane >> 4));
+            for (int i = 0; i < TB; ++i) xsc[u][i] = row_scales(p, from.s, source[i], k * 8 + (lane >> 4));
         }
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 #pragma unroll
@@ -146,71 +141,82 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
 }
 
 // ---------------------------------------------------------------- many rows
-// A workgroup of WR x WT wavefronts owns 64 * WR packed channels x 16 * TB * WT rows; a wavefront 64 x 16 TB of them.  K goes by in
-// steps of 256.  LDS holds NSW steps' weights and NSX steps' rows and scales, loaded straight into it: while a step is multiplied, the next one's
-// lie there and later ones' are on their way.  Operands are read from LDS half a step ahead, into the other half of the operand
-// registers, so one barrier a step is enough.
-// Weights lie in LDS as in memory (a wavefront's operand is 1 KiB of adjacent bytes); a row's 128 bytes are 8 blocks of 16 in the order of
-// block_at, place i stored at i ^ (row & 7), so that what an LDS cycle reads lies in different banks.
-template <int WR, int WT, int TB, int NSW, int NSX> struct Tile4 {
+// A workgroup of WR x WT wavefronts owns 64 * WR packed channels x 16 * TB * WT rows; a wavefront 64 x 16 TB of them.  K goes by in steps
+// of 256, each two halves of one matrix instruction's 128.
+// Rows go through LDS, NS steps of them, loaded straight into it: while a step is multiplied the next one's lie there and later ones' are on
+// their way; a wavefront reads the operand of 16 rows three before it is multiplied.
+// Weights go from memory into registers, three halves ahead: their layout in memory is the operands', and the wavefronts that share them read them
+// at the same time.  Through LDS as well, LDS is what bounds the loop (192 + 68 KiB a step of 256 x 256, 2080 cycles at 128 bytes, beside
+// 2048 of the matrix units).
+// A row's 128 bytes are 8 blocks of 16, block c stored at c ^ (row & 7), so that what an LDS cycle reads lies in different banks.
+template <int WR, int WT, int TB, int NS> struct Tile4 {
     static constexpr int kWaves = WR * WT, kRows = 16 * TB * WT;
-    static constexpr int kWBytes = WR * 8192, kXBytes = kRows * 128, kSBytes = WR * 512 + kRows * 8;   // of a step
-    static constexpr int kWLoads = kWBytes / 1024 / kWaves, kXLoads = kXBytes / 1024 / kWaves;         // of 1 KiB, a wavefront and step
-    static constexpr int kSUnits = kSBytes / 256, kSLoads = (kSUnits + kWaves - 1) / kWaves;           // of 256 bytes: the first load the weights'
-    static constexpr int kSPitch = kSLoads * kWaves * 256;   // (units past the scales are loaded with nothing)
-    static_assert(WT == 2, "a load of scales is of weights' or of rows' in all wavefronts");
-    static constexpr int kXAt = NSW * kWBytes, kSAt = kXAt + NSX * kXBytes, kLds = kSAt + NSX * kSPitch;
-    static_assert(TB % 4 == 0 && kWBytes % (1024 * kWaves) == 0 && kXBytes % (1024 * kWaves) == 0, "every wavefront issues the same loads");
-    static_assert(kLds <= 160 * 1024 && NSW >= NSX && NSX >= 2, "");
-    // Loads that may be out while a step waits for the stages of the next: those of later steps.  Rows are loaded first, so with more stages
-    // of weights the weights of the step that goes with the last rows may be out too.
-    static constexpr int kLoads = kWLoads + kXLoads + kSLoads;
-    static constexpr int kOut = (NSX - 2) * kLoads + (NSW > NSX ? kWLoads : 0);
+    static constexpr int kXBytes = kRows * 128, kXLoads = kXBytes / 1024 / kWaves;              // of 1 KiB, a wavefront and step
+    static constexpr int kSUnits = kRows / 32, kSLoads = (kSUnits + kWaves - 1) / kWaves;       // of 256 bytes: the rows' scales
+    static constexpr int kStage = kXBytes + kSUnits * 256, kNowhere = NS * kStage, kLds = kNowhere + 256;   // (where loads of nothing land)
+    static constexpr int kLoads = kXLoads + kSLoads;
+    static_assert(TB % 4 == 0 && kXBytes % (1024 * kWaves) == 0, "every wavefront issues the same loads");
+    static_assert(NS >= 3 && kLds <= 160 * 1024, "");
 };
 
 // The rows' scales of a tile and step as the kernel's lanes read them: [2 halves][rows / 64][64 lanes] words, byte j that of row block
 // 4 (rows / 64) + j.
 struct TileHead {
-    int tiles, pad[3];
+    int tiles, pad[3];   // of rows
 };
 struct TileRows {
     int expert, count;
     int64_t row0;
 };
 
-__global__ __launch_bounds__(256) void mx4_scales_kernel(Mx4Product p, int per, int parts, TileHead* head, TileRows* tiles, unsigned* to)
+// 64 rows of a tile a workgroup.
+__global__ __launch_bounds__(256) void mx4_scales_kernel(Mx4Product p, int per, TileHead* head, TileRows* tiles, unsigned* to)
 {
-    const int tile = blockIdx.x / parts, part = blockIdx.x - tile * parts;
-    const RowTile t = row_tile(p, tile, per);
-    if (part == 0 && threadIdx.x == 0) {
+    __shared__ int sources[64];
+    const int parts = per / 64, tile = blockIdx.x / parts, part = blockIdx.x - tile * parts;   // (blockIdx.y: of the steps)
+    int all = 0;
+    const RowTile t = row_tile(p, tile, per, blockIdx.x == 0, &all);
+    if (part == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
         tiles[tile] = {t.expert, t.count, t.row0};
-        if (p.grouped && t.count > 0) atomicMax(&head->tiles, tile + 1);
+        if (tile == 0) head->tiles = all;
     }
     if (t.count == 0) return;
-    const int first = part * 256 + threadIdx.x, words = p.steps * per * 2;
-    if (first >= words) return;
-    const int lane = first & 63, j4 = (first >> 6) % (per / 64), half = (first >> 6) / (per / 64) & 1, step = (first >> 6) / (per / 64) >> 1;
-    const int kb = step * 8 + 2 * (lane >> 4) + half;
-    const int64_t base = p.index ? 0 : t.row0;
-    unsigned word = 0;
+    if (threadIdx.x < 64) sources[threadIdx.x] = source_of(p, t, part * 64 + threadIdx.x);
+    __syncthreads();
+    const int lane = threadIdx.x & 63;
+    int src[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int src = source_of(p, t, (j4 * 4 + j) * 16 + (lane & 15));
-        unsigned s = 127;   // past the row's blocks codes of 0 are multiplied
-        if (src == -2) s = 255;
-        else if (src >= 0 && kb < p.blocks) s = p.s[(base + src) * p.lds + kb];
-        word |= s << (8 * j);
+    for (int j = 0; j < 4; ++j) src[j] = sources[j * 16 + (lane & 15)];
+    const uint8_t* from = p.s + (p.index ? 0 : t.row0) * p.lds;
+    unsigned* put = to + (int64_t)tile * p.steps * per * 2 + part * 64 + lane;
+    for (int sh = blockIdx.y * 4 + (threadIdx.x >> 6); sh < p.steps * 2; sh += gridDim.y * 4) {   // step and half
+        const int kb = sh * 4 + (lane >> 4);
+        unsigned word = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            unsigned s = 127;   // past the row's blocks codes of 0 are multiplied
+            if (src[j] == -2) s = 255;
+            else if (src[j] >= 0 && kb < p.blocks) s = from[src[j] * p.lds + kb];
+            word |= s << (8 * j);
+        }
+        put[(int64_t)sh * per] = word;
     }
-    to[(int64_t)tile * words + first] = word;
 }
-
-__global__ void mx4_head_kernel(TileHead* head) { head->tiles = 0; }
 
 // 4 bytes a lane from memory to LDS at `lds` + 4 * lane, as load_to_lds.
 __device__ inline void load_to_lds4(__amdgpu_buffer_rsrc_t r, unsigned voff, unsigned lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : :
                  "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(r));
+}
+
+// Values that are the same in all lanes, as the loads into LDS want them.
+__device__ inline int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline TileRows tile_rows(const TileRows* tiles, int i)
+{
+    const TileRows t = tiles[i];
+    const unsigned lo = (unsigned)scalar((int)t.row0), hi = (unsigned)scalar((int)(t.row0 >> 32));
+    return {scalar(t.expert), scalar(t.count), (int64_t)((unsigned long long)hi << 32 | lo)};
 }
 
 constexpr int largest_divisor4(int n, int most) { return most >= n ? n : n % most == 0 ? most : largest_divisor4(n, most - 1); }
@@ -316,11 +322,11 @@ __device__ inline void store_tile4(const Mx4Product& p, const Channels4<GATED, 4
     }
 }
 
-template <int WR, int WT, int TB, int NSW, int NSX, bool GATED, int OUT>
-__global__ __launch_bounds__(WR * WT * 64) void mx4_tile_kernel(Mx4Product p, TileOrder order, const TileHead* head, const TileRows* tiles,
-                                                               const unsigned* scales)
+template <int WR, int WT, int TB, int NS, int PER_CU, bool GATED, int OUT>
+__global__ __launch_bounds__(WR * WT * 64, PER_CU * WR * WT / 4) void mx4_tile_kernel(Mx4Product p, TileOrder order, const TileHead* head,
+                                                                                      const TileRows* tiles, const unsigned* scales)
 {
-    using T = Tile4<WR, WT, TB, NSW, NSX>;
+    using T = Tile4<WR, WT, TB, NS>;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wr = wave % WR, wt = wave / WR;
@@ -330,115 +336,111 @@ __global__ __launch_bounds__(WR * WT * 64) void mx4_tile_kernel(Mx4Product p, Ti
         if ((int)blockIdx.x >= order.tiles()) return;
     }
     order.at(blockIdx.x, tc, tr, tile, split);
-    const TileRows t = tiles[tr];
-    const int g0 = tc * WR;
-    const int ngrp = p.groups - g0 < WR ? p.groups - g0 : WR;
-    const int steps = p.steps;
-    const size_t group0 = (size_t)t.expert * p.groups + g0;
+    tc = scalar(tc);
+    tr = scalar(tr);
+    const TileRows t = tile_rows(tiles, tr);
+    const int g0 = tc * WR, steps = p.steps, halves = steps * 2;
+    const bool own = g0 + wr < p.groups;   // (a wavefront past the last group multiplies zeros)
+    const size_t group = (size_t)t.expert * p.groups + (own ? g0 + wr : 0);
     const RowTile rt{t.expert, t.count, t.row0};
-    const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + group0 * steps * 8192, (unsigned)ngrp * steps * 8192);
-    const __amdgpu_buffer_rsrc_t gsr = q8_rsrc(p.ws + group0 * steps * 128, (unsigned)ngrp * steps * 512);
+    const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + group * halves * 4096, own ? (unsigned)halves * 4096 : 0);
+    const __amdgpu_buffer_rsrc_t gsr = q8_rsrc(p.ws + group * halves * 64, own ? (unsigned)halves * 256 : 0);
     const __amdgpu_buffer_rsrc_t xsr = RowBuffers(p, rt).q;
-    const __amdgpu_buffer_rsrc_t ssr = q8_rsrc(scales + (size_t)tr * steps * T::kRows * 2, (unsigned)steps * T::kRows * 8);
+    const __amdgpu_buffer_rsrc_t ssr = q8_rsrc(scales + (size_t)tr * halves * T::kRows, (unsigned)halves * T::kRows * 4);
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem;
+    constexpr unsigned kNone = 0xc0000000u;   // (and what a lane adds: past the end of weights and scales)
     // Rows past the tile's last read its first: what comes of them is not stored.  (The scale of a row for an index outside x is NaN.)
+    const int chunk = (lane & 7) ^ (lane >> 3);   // the block of a step that the lane loads, of a row with row & 7 = lane / 8
     unsigned xvoff[T::kXLoads];
-    const int chunk = block_at((lane & 7) ^ (lane >> 3));   // the block of a step that the lane loads (row & 7 is lane >> 3)
 #pragma unroll
     for (int i = 0; i < T::kXLoads; ++i) {
-        const int row = (wave + i * T::kWaves) * 8 + (lane >> 3), src = source_of(p, rt, row);
+        const int src = source_of(p, rt, (wave + i * T::kWaves) * 8 + (lane >> 3));
         xvoff[i] = (unsigned)((src < 0 ? 0 : src) * p.ldq) + chunk * 16;
     }
-    const int xsteps = (p.blocks + 7 - chunk) >> 3;         // steps that have it
+    const int xsteps = (p.blocks + 7 - chunk) >> 3;   // steps that have it
     const unsigned lane16 = lane * 16, lane4 = lane * 4;
-    // load i of a step: rows and scales of step sx, weights of step sw; past the last step nothing is read, so that the count of loads holds
-    auto fetch = [&](int i, int sw, unsigned wat, int sx, unsigned xat, unsigned sat) {
-        constexpr unsigned kNone = 0xc0000000u;   // (and what a lane adds: past the end of weights and scales)
+    // load i of step s into the stage at `at`; past the last step nothing is read, so that the count of loads holds
+    auto fetch = [&](int i, int s, unsigned at) {
         if (i < T::kXLoads) {
-            load_to_lds(xsr, sx < xsteps ? xvoff[i] + (unsigned)sx * 128 : kPast, lds0 + T::kXAt + xat + (wave + i * T::kWaves) * 1024);
-        } else if (i == T::kXLoads) {
-            load_to_lds4(gsr, (sx < steps ? ((unsigned)((wave >> 1) * steps + sx) * 2 + (wave & 1)) * 256 : kNone) + lane4, lds0 + T::kSAt + sat + wave * 256);
-        } else if (i < T::kXLoads + T::kSLoads) {
-            const int u = wave + (i - T::kXLoads - 1) * T::kWaves;
-            load_to_lds4(ssr, (sx < steps && u < T::kRows / 32 ? (unsigned)sx * (T::kRows * 8) + u * 256 : kNone) + lane4,
-                         lds0 + T::kSAt + sat + (wave + (i - T::kXLoads) * T::kWaves) * 256);
+            load_to_lds(xsr, s < xsteps ? xvoff[i] + (unsigned)s * 128 : kPast, lds0 + at + (wave + i * T::kWaves) * 1024);
         } else {
-            const int n = i - T::kXLoads - T::kSLoads, c = wave + n * T::kWaves;   // 1 KiB of the stage
-            load_to_lds(wsr, (sw < steps ? ((unsigned)(c >> 3) * steps + sw) * 8192 + (c & 7) * 1024 : kNone) + lane16, lds0 + wat + c * 1024);
+            const int u = wave + (i - T::kXLoads) * T::kWaves;
+            const bool in = T::kSUnits % T::kWaves == 0 || u < T::kSUnits;
+            load_to_lds4(ssr, (s < steps && in ? (unsigned)s * (T::kRows * 8) + u * 256 : kNone) + lane4, lds0 + (in ? at + T::kXBytes + u * 256 : (unsigned)T::kNowhere));
         }
     };
-    const int wlane = wr * 8192 + lane * 16;
-    const int xlane = T::kXAt + (wt * TB * 16 + (lane & 15)) * 128;
-    const int slane = T::kSAt + lane * 4;
-    i32x4 f[2][4 + TB];               // operands of the two halves of a step: 4 blocks of weights, TB of rows
-    unsigned fs[2][1 + TB / 4];       // and their scales
-    constexpr int READS = 4 + TB + 1 + TB / 4;
-    auto read = [&](int h, int i, unsigned wat, unsigned xat, unsigned sat) {
-        if (i < 4) f[h][i] = *reinterpret_cast<const i32x4*>(smem + wat + wlane + h * 4096 + i * 1024);
-        else if (i < 4 + TB) f[h][i] = *reinterpret_cast<const i32x4*>(smem + xat + xlane + (((4 * h + (lane >> 4)) ^ (lane & 7)) << 4) + (i - 4) * 2048);
-        else if (i == 4 + TB) fs[h][0] = *reinterpret_cast<const unsigned*>(smem + sat + slane + wr * 512 + h * 256);
-        else fs[h][i - 4 - TB] = *reinterpret_cast<const unsigned*>(smem + sat + slane + WR * 512 + h * (T::kRows * 4) + (wt * (TB / 4) + i - 5 - TB) * 256);
+    i32x4 w[4][4], x[4];            // weights of four halves; rows of four blocks
+    unsigned ws[4], xs[2][TB / 4];  // their scales
+    auto weights = [&](int set, int i, int half) {   // load i of a half's
+        const unsigned from = half < halves ? (unsigned)half : kNone >> 12;
+        if (i < 4) w[set][i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wsr, from * 4096 + i * 1024 + lane16, 0, 0));
+        else ws[set] = __builtin_amdgcn_raw_buffer_load_b32(gsr, from * 256 + lane4, 0, 0);
     };
+    const int xlane = (wt * TB * 16 + (lane & 15)) * 128 + (((lane >> 4) ^ (lane & 7)) << 4), slane = T::kXBytes + wt * TB * 64 + lane * 4;
+    auto rows = [&](int h, int j, unsigned at) { x[j & 3] = *reinterpret_cast<const i32x4*>(smem + at + (xlane ^ (h * 64)) + j * 2048); };
+    auto row_words = [&](int h, int i, unsigned at) { xs[h][i] = *reinterpret_cast<const unsigned*>(smem + at + slane + h * (T::kRows * 4) + i * 256); };
     f32x4 acc[TB][4] = {};
-    constexpr int LOADS = T::kLoads;
 #pragma unroll
-    for (int s = 0; s < NSX; ++s)
+    for (int s = 0; s < NS; ++s) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) fetch(i, s, s * T::kWBytes, s, s * T::kXBytes, s * T::kSPitch);
+        for (int i = 0; i < T::kLoads; ++i) fetch(i, s, s * T::kStage);
+        asm volatile("" : : : "memory");   // (the first step's rows are the oldest loads)
+        if (s < 3)
 #pragma unroll
-    for (int s = NSX; s < NSW; ++s)
+            for (int i = 0; i < 5; ++i) weights(s, i, s);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((NS - 1) * T::kLoads + 15) : "memory");
 #pragma unroll
-        for (int i = T::kXLoads + T::kSLoads; i < LOADS; ++i) fetch(i, s, s * T::kWBytes, 0, 0, 0);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((NSX - 1) * LOADS + (NSW - NSX) * T::kWLoads) : "memory");
+    for (int j = 0; j < 3; ++j) rows(0, j, 0);
 #pragma unroll
-    for (int i = 0; i < READS; ++i) read(0, i, 0, 0, 0);
-    auto multiply = [&](int h, int j) {
-        const unsigned ws = fs[h][0], xs = fs[h][1 + j / 4];
+    for (int i = 0; i < TB / 4; ++i) row_words(0, i, 0);
+    auto multiply = [&](int set, int h, int j) {
         auto four = [&](auto ox) {
             constexpr int OX = decltype(ox)::value;
-            acc[j][0] = mma4<0, OX>(f[h][0], f[h][4 + j], acc[j][0], ws, xs);
-            acc[j][1] = mma4<1, OX>(f[h][1], f[h][4 + j], acc[j][1], ws, xs);
-            acc[j][2] = mma4<2, OX>(f[h][2], f[h][4 + j], acc[j][2], ws, xs);
-            acc[j][3] = mma4<3, OX>(f[h][3], f[h][4 + j], acc[j][3], ws, xs);
+            acc[j][0] = mma4<0, OX>(w[set][0], x[j & 3], acc[j][0], ws[set], xs[h][j / 4]);
+            acc[j][1] = mma4<1, OX>(w[set][1], x[j & 3], acc[j][1], ws[set], xs[h][j / 4]);
+            acc[j][2] = mma4<2, OX>(w[set][2], x[j & 3], acc[j][2], ws[set], xs[h][j / 4]);
+            acc[j][3] = mma4<3, OX>(w[set][3], x[j & 3], acc[j][3], ws[set], xs[h][j / 4]);
         };
         if (j % 4 == 0) four(std::integral_constant<int, 0>{});
         else if (j % 4 == 1) four(std::integral_constant<int, 1>{});
         else if (j % 4 == 2) four(std::integral_constant<int, 2>{});
         else four(std::integral_constant<int, 3>{});
     };
-    unsigned wnow = 0, xnow = 0, snow = 0;   // the stages that are multiplied
-    for (int k = 0; k < steps; ++k) {
-        const unsigned wnext = wnow + T::kWBytes == NSW * T::kWBytes ? 0 : wnow + T::kWBytes;
-        const unsigned xnext = xnow + T::kXBytes == NSX * T::kXBytes ? 0 : xnow + T::kXBytes;
-        const unsigned snext = snow + T::kSPitch == NSX * T::kSPitch ? 0 : snow + T::kSPitch;
-        // first half: its operands are in registers; the second half's are read meanwhile
+    unsigned now = 0;   // the stage that is multiplied
+    // two steps a turn, for the four sets of weights; past the last step zeros are multiplied
+    for (int k = 0; k < halves; k += 4) {
 #pragma unroll
-        for (int j = 0; j < TB; ++j) {
+        for (int q = 0; q < 4; ++q) {
+            const int h = q & 1;
+            const unsigned then = now + T::kStage == T::kNowhere ? 0 : now + T::kStage;
 #pragma unroll
-            for (int i = j * READS / TB; i < (j + 1) * READS / TB; ++i) read(1, i, wnow, xnow, snow);
-            multiply(0, j);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int j = 0; j < TB; ++j) {
+                // In a step's second half, once all of its rows are read: all wavefronts have read this stage, and the next one has landed.  Younger
+                // than its loads are those of NS - 2 steps and of the weights of four halves.
+                if (h == 1 && j == TB - 3)
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((NS - 2) * T::kLoads + 15) : "memory");
+                if (j + 3 < TB) rows(h, j + 3, now);
+                else rows(1 - h, j + 3 - TB, h == 0 ? now : then);
+                if (j >= TB - 3 && j - (TB - 3) < TB / 4) row_words(1 - h, j - (TB - 3), h == 0 ? now : then);
+                if constexpr (TB == 4) {
+                    weights((q + 3) & 3, j, k + q + 3);
+                    if (j == 3) weights((q + 3) & 3, 4, k + q + 3);
+                } else {
+                    if (j < 5) weights((q + 3) & 3, j, k + q + 3);
+                }
+                if (h == 1 && j >= TB - 3)
+#pragma unroll
+                    for (int i = (j - TB + 3) * T::kLoads / 3; i < (j - TB + 4) * T::kLoads / 3; ++i) fetch(i, (k + q) / 2 + NS, now);
+                multiply(q, h, j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (h == 1) now = then;
         }
-        // these stages have been read, the next ones have landed
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(T::kOut) : "memory");
-        // second half: the next step's first operands are read, and what comes after the last stages in LDS is loaded in these ones' place
-#pragma unroll
-        for (int j = 0; j < TB; ++j) {
-#pragma unroll
-            for (int i = j * READS / TB; i < (j + 1) * READS / TB; ++i) read(0, i, wnext, xnext, snext);
-#pragma unroll
-            for (int i = j * LOADS / TB; i < (j + 1) * LOADS / TB; ++i)
-                fetch(i, k + NSW, wnow, k + NSX, xnow, snow);
-            multiply(1, j);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        wnow = wnext;
-        xnow = xnext;
-        snow = snext;
     }
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // no load into LDS outlives the workgroup
     Channels4<GATED, 4> ch;
-    ch.load(p, t.expert, g0 + wr < p.groups ? g0 + wr : p.groups - 1, 0, lane);   // (what a wavefront past the last group has is not stored)
+    ch.load(p, t.expert, own ? g0 + wr : p.groups - 1, 0, lane);   // (what a wavefront past the last group has is not stored)
     constexpr int kOuts = WR * Channels4<GATED, 4>::kRuns * 32;
     constexpr int JP4 = largest_divisor4(TB, T::kLds / (16 * WT * kOuts * 4)), JP2 = largest_divisor4(TB, T::kLds / (16 * WT * kOuts * 2)),
                   JPM = largest_divisor4(TB, T::kLds / (16 * WT * kOuts / 2));
@@ -474,7 +476,7 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* q, int64_t
         const int64_t gk = i >> 9;
         const int step = (int)(gk % steps), group = (int)(gk / steps % groups);
         const int64_t expert = gk / steps / groups;
-        const int c = q8_row_of(group * 64 + b * 16 + (lane & 15), channels, gated), kb = step * 8 + 2 * (lane >> 4) + h;
+        const int c = q8_row_of(group * 64 + b * 16 + (lane & 15), channels, gated), kb = step * 8 + 4 * h + (lane >> 4);
         i32x4 v = {0, 0, 0, 0};
         if (c >= 0 && kb < blocks) v = block_codes(q + (expert * channels + c) * ldq, kb, width);
         *reinterpret_cast<i32x4*>(to + i * 16) = v;
@@ -502,7 +504,7 @@ __global__ __launch_bounds__(256) void mx4_unpack_kernel(const uint8_t* from, co
         const int64_t gk = i >> 9;
         const int step = (int)(gk % steps), group = (int)(gk / steps % groups);
         const int64_t expert = gk / steps / groups;
-        const int c = q8_row_of(group * 64 + b * 16 + (lane & 15), channels, gated), kb = step * 8 + 2 * (lane >> 4) + h;
+        const int c = q8_row_of(group * 64 + b * 16 + (lane & 15), channels, gated), kb = step * 8 + 4 * h + (lane >> 4);
         if (c < 0 || kb >= blocks) continue;
         const int64_t row = expert * channels + c;
         *reinterpret_cast<i32x4*>(q + (row * blocks + kb) * 16) = *reinterpret_cast<const i32x4*>(from + i * 16);
@@ -548,41 +550,36 @@ int pick_few4(const Mx4Product& p, hipStream_t s)
 
 // The tile kernels' shapes.
 struct Shape4 {
-    int wr, rows, waves;
+    int wr, rows, waves, per_cu;   // per_cu: workgroups that a CU holds (by LDS)
 };
-constexpr Shape4 kShapes4[] = {{4, 256, 8},    // 256 packed channels x 256 rows
-                               {4, 128, 8},
-                               {2, 128, 4}};
+constexpr Shape4 kShapes4[] = {{4, 256, 8, 1},    // 256 packed channels x 256 rows
+                               {4, 128, 4, 2},
+                               {4, 64, 4, 2}};
 
-template <int SHAPE, int WT, int TB, int NSW, int NSX, bool GATED, int OUT>
+template <int SHAPE, int WT, int TB, int NS, bool GATED, int OUT>
 int launch_tile4(const Mx4Product& p, const Mx4Plan& pl, char* workspace, hipStream_t s)
 {
     constexpr int WR = kShapes4[SHAPE].wr;
-    using T = Tile4<WR, WT, TB, NSW, NSX>;
+    using T = Tile4<WR, WT, TB, NS>;
     static_assert(T::kWaves == kShapes4[SHAPE].waves && T::kRows == kShapes4[SHAPE].rows, "kShapes4 describes the kernels");
     TileOrder o;
     o.splits = 1;
     o.tiles_c = (p.groups + WR - 1) / WR;
     o.tiles_r = (int)pl.tiles;
-    const int64_t grid = pl.tiles * o.tiles_c;
-    const int parts = (p.steps * T::kRows * 2 + 255) / 256;
+    const int64_t grid = pl.tiles * o.tiles_c, parts = T::kRows / 64;
     if (grid > 0x7fffffff || pl.tiles * parts > 0x7fffffff) {
-        set_error("%lld workgroups: too many", (long long)(grid > pl.tiles * parts ? grid : pl.tiles * parts));
+        set_error("%lld tiles: too many", (long long)grid);
         return NM_ERR_SHAPE;
     }
     TileHead* head = (TileHead*)workspace;
     TileRows* tiles = (TileRows*)(head + 1);
     unsigned* scales = (unsigned*)(workspace + pl.tile_bytes);
-    if (p.grouped) {
-        hipLaunchKernelGGL(mx4_head_kernel, dim3(1), dim3(1), 0, s, head);
-        NM_HIP_CHECK(hipGetLastError());
-    }
-    hipLaunchKernelGGL(mx4_scales_kernel, dim3((unsigned)(pl.tiles * parts)), dim3(256), 0, s, p, T::kRows, parts, head, tiles, scales);
+    hipLaunchKernelGGL(mx4_scales_kernel, dim3((unsigned)(pl.tiles * parts), (unsigned)(p.steps < 32 ? (p.steps + 1) / 2 : 16)), dim3(256), 0, s, p, T::kRows, head, tiles, scales);
     NM_HIP_CHECK(hipGetLastError());
     static unsigned long long done = 0;
-    const int rc = allow_lds((const void*)mx4_tile_kernel<WR, WT, TB, NSW, NSX, GATED, OUT>, T::kLds, &done);
+    const int rc = allow_lds((const void*)mx4_tile_kernel<WR, WT, TB, NS, kShapes4[SHAPE].per_cu, GATED, OUT>, T::kLds, &done);
     if (rc != NM_OK) return rc;
-    hipLaunchKernelGGL((mx4_tile_kernel<WR, WT, TB, NSW, NSX, GATED, OUT>), dim3((unsigned)grid), dim3(T::kWaves * 64), T::kLds, s, p, o,
+    hipLaunchKernelGGL((mx4_tile_kernel<WR, WT, TB, NS, kShapes4[SHAPE].per_cu, GATED, OUT>), dim3((unsigned)grid), dim3(T::kWaves * 64), T::kLds, s, p, o,
                        (const TileHead*)head, (const TileRows*)tiles, (const unsigned*)scales);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
@@ -592,9 +589,9 @@ template <bool GATED, int OUT>
 int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, char* workspace, hipStream_t s)
 {
     switch (pl.shape) {
-    case 0: return launch_tile4<0, 2, 8, 2, 2, GATED, OUT>(p, pl, workspace, s);
-    case 1: return launch_tile4<1, 2, 4, 3, 3, GATED, OUT>(p, pl, workspace, s);
-    default: return launch_tile4<2, 2, 4, 2, 2, GATED, OUT>(p, pl, workspace, s);
+    case 0: return launch_tile4<0, 2, 8, 3, GATED, OUT>(p, pl, workspace, s);
+    case 1: return launch_tile4<1, 1, 8, 3, GATED, OUT>(p, pl, workspace, s);
+    default: return launch_tile4<2, 1, 4, 4, GATED, OUT>(p, pl, workspace, s);
     }
 }
 
@@ -610,7 +607,7 @@ Mx4Plan mx4_plan(const Mx4Product& p)
     const int per = kShapes4[pl.shape].rows;
     pl.tiles = tiles_of(p, per);
     pl.tile_bytes = (sizeof(TileHead) + (size_t)pl.tiles * sizeof(TileRows) + 255) / 256 * 256;
-    pl.scale_bytes = (size_t)pl.tiles * p.steps * per * 8;
+    pl.scale_bytes = (size_t)pl.tiles * per * p.steps * 8;
     return pl;
 }
 
