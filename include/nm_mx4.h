@@ -94,15 +94,12 @@ int nm_mx4_export(const nm_mx4_t* w, uint8_t* q_host, uint8_t* scales_host);
  *   bias_dev        fp32 [channels] (gated: gates first, as the weights), or NULL
  *   residual_dev    rows of y_dtype at stride ldr, or NULL.  It may be y_dev itself (same stride).
  *   y_dev           rows of y_dtype at stride ldy (NM_MX4: codes; y_scales_dev at stride ldys, otherwise NULL)
- *   workspace_dev   at least nm_mx4_workspace() bytes, 16-byte aligned; its contents need not be kept between calls.
- *                   Calls that overlap in time need one each.
- * Errors: NM_ERR_ARG (also: workspace too small), NM_ERR_SHAPE, NM_ERR_UNSUPPORTED (a residual with gated weights or with
+ * Errors: NM_ERR_ARG, NM_ERR_SHAPE, NM_ERR_UNSUPPORTED (a residual with gated weights or with
  * an output in MX4; weights of several experts), NM_ERR_HIP.
  */
 int nm_linear_mx4(const uint8_t* q_dev, int64_t ldq, const uint8_t* scales_dev, int64_t lds, int64_t rows, int width,
                   const nm_mx4_t* w, const float* bias_dev, const void* residual_dev, int64_t ldr, void* y_dev,
-                  nm_dtype_t y_dtype, int64_t ldy, uint8_t* y_scales_dev, int64_t ldys, void* workspace_dev,
-                  size_t workspace_bytes, void* hip_stream);
+                  nm_dtype_t y_dtype, int64_t ldy, uint8_t* y_scales_dev, int64_t ldys, void* hip_stream);
 
 /*
  * nm_experts_mx4 -- products grouped by expert: row r of y, for offsets[e] <= r < offsets[e + 1], is the formula of
@@ -118,12 +115,7 @@ int nm_linear_mx4(const uint8_t* q_dev, int64_t ldq, const uint8_t* scales_dev, 
 int nm_experts_mx4(const uint8_t* q_dev, int64_t ldq, const uint8_t* scales_dev, int64_t lds, int64_t rows, int width,
                    const nm_mx4_t* w, const int32_t* offsets_dev, const int32_t* index_dev, int64_t entries,
                    const float* bias_dev, void* y_dev, nm_dtype_t y_dtype, int64_t ldy, uint8_t* y_scales_dev, int64_t ldys,
-                   void* workspace_dev, size_t workspace_bytes, void* hip_stream);
-
-/* Bytes of workspace that nm_linear_mx4 (grouped = 0) or nm_experts_mx4 (grouped = 1) needs for so many rows of y.  0 for
- * nm_linear_mx4 of up to NM_MX4_FEW_ROWS rows. */
-enum { NM_MX4_FEW_ROWS = 64 };
-int nm_mx4_workspace(int64_t rows, const nm_mx4_t* w, int grouped, size_t* bytes);
+                   void* hip_stream);
 
 /*
  * The calls above with their arguments in one block, for bindings that pay for every argument (as nm_conv2d_args).  dtype is
@@ -162,9 +154,8 @@ typedef struct nm_product_mx4_args {
     const int32_t* index_dev;
     void* y_dev;
     uint8_t* y_scales_dev;
-    void* workspace_dev;
     void* hip_stream;
-    int64_t dtype, rows, width, ldq, lds, ldr, entries, ldy, ldys, workspace_bytes;
+    int64_t dtype, rows, width, ldq, lds, ldr, entries, ldy, ldys;
 } nm_product_mx4_args_t;
 int nm_product_mx4_args(const nm_product_mx4_args_t* args);
 

@@ -16,7 +16,7 @@ import numpy as np
 
 NM_F32, NM_BF16, NM_F8E4M3, NM_I8, NM_MX4 = 0, 1, 2, 3, 4
 NM_Q8_MAX_WIDTH, NM_Q8_FEW_ROWS = 65536, 64
-NM_MX4_MAX_WIDTH, NM_MX4_MAX_EXPERTS, NM_MX4_FEW_ROWS = 65536, 1024, 64
+NM_MX4_MAX_WIDTH, NM_MX4_MAX_EXPERTS = 65536, 1024
 NM_ROUTE_MAX_EXPERTS, NM_ROUTE_MAX_CHOICES = 1024, 64
 NM_OK = 0
 NM_ERR_ARG, NM_ERR_SHAPE, NM_ERR_UNSUPPORTED, NM_ERR_ALLOC, NM_ERR_HIP, NM_ERR_IO = -1, -2, -3, -4, -5, -6
@@ -99,9 +99,8 @@ def lib():
         L.nm_mx4_free.argtypes = [vp]
         L.nm_mx4_dims.argtypes = [vp, pi, pi, pi, pi]
         L.nm_mx4_export.argtypes = [vp, vp, vp]
-        L.nm_linear_mx4.argtypes = [vp, i64, vp, i64, i64, ci, vp, vp, vp, i64, vp, ci, i64, vp, i64, vp, st, vp]
-        L.nm_experts_mx4.argtypes = [vp, i64, vp, i64, i64, ci, vp, vp, vp, i64, vp, vp, ci, i64, vp, i64, vp, st, vp]
-        L.nm_mx4_workspace.argtypes = [i64, vp, ci, ctypes.POINTER(st)]
+        L.nm_linear_mx4.argtypes = [vp, i64, vp, i64, i64, ci, vp, vp, vp, i64, vp, ci, i64, vp, i64, vp]
+        L.nm_experts_mx4.argtypes = [vp, i64, vp, i64, i64, ci, vp, vp, vp, i64, vp, vp, ci, i64, vp, i64, vp]
         L.nm_route.argtypes = [vp, ci, i64, ci, i64, ci, ci, vp, vp, vp, vp, vp, vp, st, vp]
         L.nm_route_workspace.argtypes = [i64, ci, ctypes.POINTER(st)]
         L.nm_combine.argtypes = [vp, ci, i64, i64, vp, vp, i64, ci, ci, vp, i64, vp, ci, i64, vp]
@@ -115,7 +114,7 @@ def lib():
                      "nm_force_variant", "nm_variant_legal", "nm_quantize_q8", "nm_dequantize_q8", "nm_rmsnorm_q8",
                      "nm_q8_pack", "nm_q8_free", "nm_q8_dims", "nm_q8_export", "nm_linear_q8", "nm_linear_q8_workspace", "nm_rows_q8_args",
                      "nm_dequantize_q8_args", "nm_linear_q8_args", "nm_quantize_mx4", "nm_dequantize_mx4", "nm_rmsnorm_mx4", "nm_mx4_pack",
-                     "nm_mx4_free", "nm_mx4_dims", "nm_mx4_export", "nm_linear_mx4", "nm_experts_mx4", "nm_mx4_workspace", "nm_route",
+                     "nm_mx4_free", "nm_mx4_dims", "nm_mx4_export", "nm_linear_mx4", "nm_experts_mx4", "nm_route",
                      "nm_route_workspace", "nm_combine", "nm_rows_mx4_args", "nm_dequantize_mx4_args", "nm_product_mx4_args", "nm_route_args",
                      "nm_combine_args"):
             getattr(L, name).restype = ci
@@ -688,7 +687,7 @@ def nm_linear_q8(q, scales, w: Q8Weights, bias=None, residual=None, dtype=None, 
 # Rows in MX4 are two uint8 tensors: codes [..., 16 B] and scales [..., B], with B = ceil(width / 32) blocks a row.
 _ROWS4_ARGS = struct.Struct("16qd")        # nm_rows_mx4_args_t
 _DEQUANTIZE4_ARGS = struct.Struct("10q")   # nm_dequantize_mx4_args_t
-_PRODUCT4_ARGS = struct.Struct("21q")      # nm_product_mx4_args_t
+_PRODUCT4_ARGS = struct.Struct("19q")      # nm_product_mx4_args_t
 _ROUTE_ARGS = struct.Struct("15q")         # nm_route_args_t
 _COMBINE_ARGS = struct.Struct("15q")       # nm_combine_args_t
 
@@ -877,18 +876,8 @@ def _mx4_product(q, scales, w: MX4Weights, offsets, index, bias, residual, dtype
     if residual is not None:
         ldr, rptr = _q8_stride(residual, "residual", shape, y.dtype, dev), residual.data_ptr()
     handle = w.handle.value if w.handle else 0
-    wptr = nbytes = 0
-    if optr or rows > NM_MX4_FEW_ROWS:   # (else none is needed)
-        need = ctypes.c_size_t(0)
-        rc = L.nm_mx4_workspace(rows, handle, 1 if optr else 0, ctypes.byref(need))
-        if rc < 0:
-            _check(rc)
-        nbytes = need.value
-        if nbytes:
-            ws = q.new_empty(nbytes)
-            wptr = ws.data_ptr()
-    rc = L.nm_product_mx4_args(_PRODUCT4_ARGS.pack(q.data_ptr(), scales.data_ptr(), handle, bptr, rptr, optr, iptr, y.data_ptr(), sptr, wptr,
-                                                   _q8_stream(dev), code, sources, w.width, ldq, lds, ldr, rows, ldy, ldys, nbytes))
+    rc = L.nm_product_mx4_args(_PRODUCT4_ARGS.pack(q.data_ptr(), scales.data_ptr(), handle, bptr, rptr, optr, iptr, y.data_ptr(), sptr,
+                                                   _q8_stream(dev), code, sources, w.width, ldq, lds, ldr, rows, ldy, ldys))
     if rc < 0:
         _check(rc)
     return (y, y_scales) if rounded else y

@@ -128,7 +128,7 @@ Mx4Product shape_of(const nm_mx4* w, int64_t rows, bool grouped)
 
 int product_call(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t lds, int64_t sources, int width, const nm_mx4_t* w, bool grouped,
                  const int32_t* offsets, const int32_t* index, int64_t rows, const float* bias, const void* res, int64_t ldr, void* y,
-                 nm_dtype_t dt, int64_t ldy, uint8_t* ys, int64_t ldys, void* workspace, size_t workspace_bytes, void* stream)
+                 nm_dtype_t dt, int64_t ldy, uint8_t* ys, int64_t ldys, void* stream)
 {
     if (!w) {
         set_error("null handle");
@@ -212,20 +212,7 @@ int product_call(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t l
     p.sources = (int)sources;
     p.out = dt;
     p.past = sy.rows * sy.width * (int64_t)es > ((int64_t)160 << 20);
-    const Mx4Plan plan = mx4_plan(p);
-    const size_t need = plan.bytes();
-    if (need) {
-        if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16) {
-            set_error("this call needs %zu bytes of workspace, 16-byte aligned; %zu were given", need,
-                      workspace ? workspace_bytes : (size_t)0);
-            return NM_ERR_ARG;
-        }
-        const Span sw{workspace, 1, 1, (int64_t)need, (int64_t)need};
-        for (int i = 0; i < 6; ++i) NM_TRY(check_apart("workspace", sw, names[i], *ins[i], false));
-        NM_TRY(check_apart("workspace", sw, "y", sy, false));
-        NM_TRY(check_apart("workspace", sw, "y_scales", sys, false));
-    }
-    return run_mx4_product(p, plan, workspace, (hipStream_t)stream);
+    return run_mx4_product(p, (hipStream_t)stream);
 }
 
 // The integers of a block are 64 bits wide; one that does not fit an int is out of range for every argument that is one.
@@ -368,28 +355,18 @@ int nm_mx4_export(const nm_mx4_t* w, uint8_t* q_host, uint8_t* scales_host)
     return NM_OK;
 }
 
-int nm_mx4_workspace(int64_t rows, const nm_mx4_t* w, int grouped, size_t* bytes)
-{
-    if (!w || !bytes) return null_block();
-    NM_TRY(check_rows(rows, w->width));
-    *bytes = rows ? mx4_plan(shape_of(w, rows, grouped != 0)).bytes() : 0;
-    return NM_OK;
-}
-
 int nm_linear_mx4(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t lds, int64_t rows, int width, const nm_mx4_t* w,
                   const float* bias, const void* res, int64_t ldr, void* y, nm_dtype_t dt, int64_t ldy, uint8_t* ys, int64_t ldys,
-                  void* workspace, size_t workspace_bytes, void* stream)
+                  void* stream)
 {
-    return product_call(q, ldq, scales, lds, rows, width, w, false, nullptr, nullptr, rows, bias, res, ldr, y, dt, ldy, ys, ldys, workspace,
-                        workspace_bytes, stream);
+    return product_call(q, ldq, scales, lds, rows, width, w, false, nullptr, nullptr, rows, bias, res, ldr, y, dt, ldy, ys, ldys, stream);
 }
 
 int nm_experts_mx4(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t lds, int64_t rows, int width, const nm_mx4_t* w,
                    const int32_t* offsets, const int32_t* index, int64_t entries, const float* bias, void* y, nm_dtype_t dt, int64_t ldy,
-                   uint8_t* ys, int64_t ldys, void* workspace, size_t workspace_bytes, void* stream)
+                   uint8_t* ys, int64_t ldys, void* stream)
 {
-    return product_call(q, ldq, scales, lds, rows, width, w, true, offsets, index, entries, bias, nullptr, 0, y, dt, ldy, ys, ldys, workspace,
-                        workspace_bytes, stream);
+    return product_call(q, ldq, scales, lds, rows, width, w, true, offsets, index, entries, bias, nullptr, 0, y, dt, ldy, ys, ldys, stream);
 }
 
 int nm_route_workspace(int64_t tokens, int experts, size_t* bytes)
@@ -500,10 +477,9 @@ int nm_product_mx4_args(const nm_product_mx4_args_t* a)
     if (!a) return null_block();
     if (a->offsets_dev)
         return nm_experts_mx4(a->q_dev, a->ldq, a->scales_dev, a->lds, a->rows, narrow(a->width), a->w, a->offsets_dev, a->index_dev, a->entries,
-                              a->bias_dev, a->y_dev, narrow(a->dtype), a->ldy, a->y_scales_dev, a->ldys, a->workspace_dev,
-                              size_of(a->workspace_bytes), a->hip_stream);
+                              a->bias_dev, a->y_dev, narrow(a->dtype), a->ldy, a->y_scales_dev, a->ldys, a->hip_stream);
     return nm_linear_mx4(a->q_dev, a->ldq, a->scales_dev, a->lds, a->rows, narrow(a->width), a->w, a->bias_dev, a->residual_dev, a->ldr, a->y_dev,
-                         narrow(a->dtype), a->ldy, a->y_scales_dev, a->ldys, a->workspace_dev, size_of(a->workspace_bytes), a->hip_stream);
+                         narrow(a->dtype), a->ldy, a->y_scales_dev, a->ldys, a->hip_stream);
 }
 
 int nm_route_args(const nm_route_args_t* a)

@@ -53,16 +53,7 @@ struct Mx4Product {
     nm_dtype_t out;       // NM_F32, NM_BF16 or NM_MX4
     int past;             // y is stored past the last-level cache
 };
-// What runs a call: a tile shape, or the few-row kernels (-1); and the workspace: what the tiles are, and the rows' scales as the tile
-// kernels read them.
-struct Mx4Plan {
-    int shape = -1;
-    int64_t tiles = 0;   // of rows, at most
-    size_t tile_bytes = 0, scale_bytes = 0;
-    size_t bytes() const { return tile_bytes + scale_bytes; }
-};
-Mx4Plan mx4_plan(const Mx4Product& p);
-int run_mx4_product(const Mx4Product& p, const Mx4Plan& plan, void* workspace, hipStream_t s);
+int run_mx4_product(const Mx4Product& p, hipStream_t s);
 
 // routing (nm_experts.hip)
 struct Route {

@@ -18,55 +18,66 @@ __device__ inline f32x4 mma4(i32x4 w, i32x4 x, f32x4 acc, unsigned ws, unsigned 
 
 // Rows of y that a workgroup has, and whose weights they meet.
 struct RowTile {
-    int expert, count;
-    int64_t row0;
+    int expert, count, row0;
 };
 
-// Tile number `tile` of `per` rows: the groups' tiles follow one another.  Every wavefront looks for itself, 64 groups at a time.
-// count is 0 past the last group's last tile.  `to_end`: all groups are looked at, and *all gets the number of tiles that there are.
-__device__ inline RowTile row_tile(const Mx4Product& p, int tile, int per, bool to_end = false, int* all = nullptr)
-{
-    if (!p.grouped) {
-        const int64_t row0 = (int64_t)tile * per;
-        if (to_end) *all = (int)((p.rows + (int64_t)per - 1) / per);
-        return {0, (int)(p.rows - row0 < per ? p.rows - row0 : per), row0};
+// The tiles of `per` rows that the groups have, one group's after another's.  A lane looks at (experts + 63) / 64 adjacent groups; every
+// wavefront for itself.
+struct GroupTiles {
+    int per, each, mine, upto;   // groups of a lane; tiles of its groups, and of those and all before
+    int all;
+
+    // (values outside the rows of y count as the nearer end)
+    static __device__ inline int begin(const Mx4Product& p, int e) { return e < p.experts ? min(max(p.offsets[e], 0), p.rows) : 0; }
+    static __device__ inline int rows(const Mx4Product& p, int e) { return e < p.experts ? max(min(max(p.offsets[e + 1], 0), p.rows) - begin(p, e), 0) : 0; }
+    __device__ inline GroupTiles(const Mx4Product& p, int tile_rows) : per(tile_rows), each((p.experts + 63) >> 6)
+    {
+        const int lane = threadIdx.x & 63;
+        int m = 0, to = 0, n = (int)((p.rows + (int64_t)tile_rows - 1) / tile_rows);
+        if (p.grouped) {
+#pragma unroll 4
+            for (int i = 0; i < each; ++i) m += (rows(p, lane * each + i) + tile_rows - 1) / tile_rows;
+            to = m;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int up = __shfl_up(to, d);
+                to += lane >= d ? up : 0;
+            }
+            n = __builtin_amdgcn_readlane(to, 63);
+        }
+        mine = m;
+        upto = to;
+        all = n;
     }
-    const int lane = threadIdx.x & 63;
-    RowTile found{0, 0, 0};
-    int before = 0;
-    for (int e0 = 0; e0 < p.experts; e0 += 64) {
-        const int e = e0 + lane;
-        int from = 0, n = 0;
-        if (e < p.experts) {   // (values outside the rows of y count as the nearer end)
-            from = min(max(p.offsets[e], 0), p.rows);
-            n = max(min(max(p.offsets[e + 1], 0), p.rows) - from, 0);
+    // Tile number `tile`; count is 0 past the last one.
+    __device__ inline RowTile at(const Mx4Product& p, int tile) const
+    {
+        int expert = 0, row0 = tile * per, count = max(min(p.rows - row0, per), 0);
+        if (p.grouped) {
+            int before = upto - mine;
+            count = 0;
+            for (int i = 0; i < each; ++i) {   // (every lane as if the tile were of its groups)
+                const int e = (threadIdx.x & 63) * each + i, n = rows(p, e), in = tile - before;
+                const bool here = in >= 0 && in * (int64_t)per < n;
+                expert = here ? e : expert;
+                row0 = here ? begin(p, e) + in * per : row0;
+                count = here ? min(n - in * per, per) : count;
+                before += (n + per - 1) / per;
+            }
+            const int l = tile < all ? __ffsll(__ballot(upto > tile)) - 1 : 0;
+            expert = __builtin_amdgcn_readlane(expert, l);
+            row0 = __builtin_amdgcn_readlane(row0, l);
+            count = tile < all ? __builtin_amdgcn_readlane(count, l) : 0;
         }
-        const int tiles = (n + per - 1) / per;
-        int to = tiles;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(to, d);
-            if (lane >= d) to += up;
-        }
-        const int here = __builtin_amdgcn_readlane(to, 63);
-        if (found.count == 0 && tile < before + here) {
-            const int l = __ffsll(__ballot(before + to > tile)) - 1;
-            const int in = __builtin_amdgcn_readfirstlane(tile - before - (__shfl(to, l) - __shfl(tiles, l)));
-            const int left = __builtin_amdgcn_readfirstlane(__shfl(n, l)) - in * per;
-            found = {e0 + l, left < per ? left : per, (int64_t)__builtin_amdgcn_readfirstlane(__shfl(from, l)) + (int64_t)in * per};
-            if (!to_end) return found;
-        }
-        before += here;
+        return {__builtin_amdgcn_readfirstlane(expert), __builtin_amdgcn_readfirstlane(count), __builtin_amdgcn_readfirstlane(row0)};
     }
-    if (to_end) *all = before;
-    return found;
-}
+};
 
 // Where row `row` of a tile comes from: rows of x from `base` on that the kernels' buffers begin with.  -1: nowhere.
 __device__ inline int source_of(const Mx4Product& p, const RowTile& t, int row)
 {
     if (row >= t.count) return -1;
     if (!p.index) return row;
-    const int at = p.index[t.row0 + row];
+    const int at = p.index[(int64_t)t.row0 + row];
     return (unsigned)at < (unsigned)p.sources ? at : -2;   // -2: an index outside x
 }
 
@@ -218,5 +229,21 @@ __device__ inline void emit4(const Mx4Product& p, const Channels4<GATED, NB>& ch
         else store(std::false_type{});
     }
 }
+
+// Tile of a workgroup.  Workgroups go to the eight XCDs, each with an L2 of its own, in turn by their number: every XCD gets a run of
+// adjacent tiles, in bands of `band` tiles of rows, whose weights it reads once.
+struct TileBands {
+    int tiles_c, tiles_r, band;
+    __host__ __device__ inline int tiles() const { return tiles_c * tiles_r; }
+    __device__ inline void at(int block, int& tc, int& tr) const
+    {
+        const int n = tiles(), xcd = block & 7, more = n & 7;
+        const int tile = xcd * (n >> 3) + (xcd < more ? xcd : more) + (block >> 3);
+        const int b = tile / (band * tiles_c), in = tile - b * band * tiles_c;
+        const int h = tiles_r - b * band < band ? tiles_r - b * band : band;
+        tc = in / h;
+        tr = b * band + in % h;
+    }
+};
 
 }  // namespace nm

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int tile = blockIdx.x / parts, b0 = (blockIdx.x - tile * parts) * RB;   // (RB divides 4: a workgroup stays within its row group)
-    const RowTile t = row_tile(p, tile, 16 * TB);
+    const RowTile t = GroupTiles(p, 16 * TB).at(p, tile);
     if (t.count == 0) return;
     const size_t group = (size_t)t.expert * p.groups + (b0 >> 2);
     const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + group * p.steps * 8192, (unsigned)p.steps * 8192);
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
 #pragma unroll
                 for (int n = 1; n < NW; ++n) sum[b] += part[((n * TB + j) * RB + i + b) * 64 + lane];
             }
-            emit4<GATED, NB>(p, ch, sum, t.row0 + row, row < t.count);
+            emit4<GATED, NB>(p, ch, sum, (int64_t)t.row0 + row, row < t.count);
         }
     };
     using One = std::integral_constant<int, 1>;
@@ -141,96 +141,42 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
 }
 
 // ---------------------------------------------------------------- many rows
-// A workgroup of WR x WT wavefronts owns 64 * WR packed channels x 16 * TB * WT rows; a wavefront 64 x 16 TB of them.  K goes by in steps
+// A workgroup of WR wavefronts owns 64 * WR packed channels x 16 * TB rows; a wavefront 64 x 16 TB of them.  K goes by in steps
 // of 256, each two halves of one matrix instruction's 128.
 // Rows go through LDS, NS steps of them, loaded straight into it: while a step is multiplied the next one's lie there and later ones' are on
 // their way; a wavefront reads the operand of 16 rows three before it is multiplied.
-// Weights go from memory into registers, three halves ahead: their layout in memory is the operands', and the wavefronts that share them read them
-// at the same time.  Through LDS as well, LDS is what bounds the loop (192 + 68 KiB a step of 256 x 256, 2080 cycles at 128 bytes, beside
-// 2048 of the matrix units).
+// Weights go from memory into registers, three halves ahead: their layout in memory is the operands', and no other wavefront of the workgroup
+// wants them.  Through LDS as well, LDS is what bounds the loop.
+// The rows' scales are dealt out in LDS for kSteps steps at once, as the lanes read them: a word has those of four blocks of 16 rows.
+// (Read byte by byte in the loop they made large products 3 to 8 % slower, dealt out by a kernel in front small ones 2 to 5 us.)
 // A row's 128 bytes are 8 blocks of 16, block c stored at c ^ (row & 7), so that what an LDS cycle reads lies in different banks.
-template <int WR, int WT, int TB, int NS> struct Tile4 {
-    static constexpr int kWaves = WR * WT, kRows = 16 * TB * WT;
-    static constexpr int kXBytes = kRows * 128, kXLoads = kXBytes / 1024 / kWaves;              // of 1 KiB, a wavefront and step
-    static constexpr int kSUnits = kRows / 32, kSLoads = (kSUnits + kWaves - 1) / kWaves;       // of 256 bytes: the rows' scales
-    static constexpr int kStage = kXBytes + kSUnits * 256, kNowhere = NS * kStage, kLds = kNowhere + 256;   // (where loads of nothing land)
-    static constexpr int kLoads = kXLoads + kSLoads;
-    static_assert(TB % 4 == 0 && kXBytes % (1024 * kWaves) == 0, "every wavefront issues the same loads");
+template <int WR, int TB, int NS> struct Tile4 {
+    static constexpr int kWaves = WR, kThreads = 64 * kWaves, kRows = 16 * TB;
+    static constexpr int kXBytes = kRows * 128, kXLoads = kXBytes / 1024 / kWaves;       // of 1 KiB, a wavefront and step
+    static constexpr int kSteps = 24, kWords = kRows / 64;                               // words of scales of a half and lane
+    static constexpr int kHalf = kWords * 256 + 4;                                       // (so that a row's words go to different banks)
+    static constexpr int kSAt = NS * kXBytes, kFromAt = kSAt + (kSteps * 2 + 1) * kHalf; // (a half past the last is read)
+    static constexpr int kLds = kFromAt + kRows * 4;                                     // where the tile's rows lie in x, for an index
+    static_assert(TB % 4 == 0 && kXBytes % (1024 * kWaves) == 0 && kThreads % 32 == 0 && 16 * kWords % (kThreads / 32) == 0, "every wavefront issues the same loads");
     static_assert(NS >= 3 && kLds <= 160 * 1024, "");
 };
 
-// The rows' scales of a tile and step as the kernel's lanes read them: [2 halves][rows / 64][64 lanes] words, byte j that of row block
-// 4 (rows / 64) + j.
-struct TileHead {
-    int tiles, pad[3];   // of rows
-};
-struct TileRows {
-    int expert, count;
-    int64_t row0;
-};
-
-// 64 rows of a tile a workgroup.
-__global__ __launch_bounds__(256) void mx4_scales_kernel(Mx4Product p, int per, TileHead* head, TileRows* tiles, unsigned* to)
-{
-    __shared__ int sources[64];
-    const int parts = per / 64, tile = blockIdx.x / parts, part = blockIdx.x - tile * parts;   // (blockIdx.y: of the steps)
-    int all = 0;
-    const RowTile t = row_tile(p, tile, per, blockIdx.x == 0, &all);
-    if (part == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-        tiles[tile] = {t.expert, t.count, t.row0};
-        if (tile == 0) head->tiles = all;
-    }
-    if (t.count == 0) return;
-    if (threadIdx.x < 64) sources[threadIdx.x] = source_of(p, t, part * 64 + threadIdx.x);
-    __syncthreads();
-    const int lane = threadIdx.x & 63;
-    int src[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) src[j] = sources[j * 16 + (lane & 15)];
-    const uint8_t* from = p.s + (p.index ? 0 : t.row0) * p.lds;
-    unsigned* put = to + (int64_t)tile * p.steps * per * 2 + part * 64 + lane;
-    for (int sh = blockIdx.y * 4 + (threadIdx.x >> 6); sh < p.steps * 2; sh += gridDim.y * 4) {   // step and half
-        const int kb = sh * 4 + (lane >> 4);
-        unsigned word = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            unsigned s = 127;   // past the row's blocks codes of 0 are multiplied
-            if (src[j] == -2) s = 255;
-            else if (src[j] >= 0 && kb < p.blocks) s = from[src[j] * p.lds + kb];
-            word |= s << (8 * j);
-        }
-        put[(int64_t)sh * per] = word;
-    }
-}
-
-// 4 bytes a lane from memory to LDS at `lds` + 4 * lane, as load_to_lds.
-__device__ inline void load_to_lds4(__amdgpu_buffer_rsrc_t r, unsigned voff, unsigned lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : :
-                 "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(r));
-}
-
-// Values that are the same in all lanes, as the loads into LDS want them.
+// A value that is the same in all lanes, as the loads into LDS want it.
 __device__ inline int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ inline TileRows tile_rows(const TileRows* tiles, int i)
-{
-    const TileRows t = tiles[i];
-    const unsigned lo = (unsigned)scalar((int)t.row0), hi = (unsigned)scalar((int)(t.row0 >> 32));
-    return {scalar(t.expert), scalar(t.count), (int64_t)((unsigned long long)hi << 32 | lo)};
-}
 
 constexpr int largest_divisor4(int n, int most) { return most >= n ? n : n % most == 0 ? most : largest_divisor4(n, most - 1); }
 
 // A workgroup's outputs through LDS, so that whole rows of its tile are stored, 16 bytes a thread and adjacent threads adjacent.  JP of
 // the TB blocks of rows at a time, STAGE32 in fp32 (fp32 outputs, and for a residual, so that it rounds once), or as what is stored.  The
-// 16-byte pieces of a row lie at piece ^ (row & 7) (fewer bits for rows of fewer pieces).
-template <int WR, int WT, int TB, int JP, bool STAGE32, bool GATED, int OUT>
-__device__ inline void store_tile4(const Mx4Product& p, const Channels4<GATED, 4>& ch, const f32x4 (&acc)[TB][4], char* smem,
-                                   int wr, int wt, int lane, int group0, const TileRows& t)
+// 16-byte pieces of a row lie at piece ^ (row & 7) (fewer bits for rows of fewer pieces).  (Codes in MX4 stored straight from the registers,
+// 16 bytes of a row an instruction, made 4096 x 4096 -> 2 x 12288 8 % slower.)
+template <int WR, int TB, int JP, bool STAGE32, bool GATED, int OUT>
+__device__ inline void store_tile4(const Mx4Product& p, const Channels4<GATED, 4>& ch, const f32x4 (&acc)[TB][4], char* smem, int wave,
+                                   int lane, int group0, const RowTile& t)
 {
     constexpr bool MX = OUT == NM_MX4, BF16 = OUT == NM_BF16;
     constexpr int C = Channels4<GATED, 4>::kRuns * 8;   // outputs of a group and lane
-    constexpr int kOuts = WR * C * 4, kThreads = WR * WT * 64, kRows = WT * JP * 16;
+    constexpr int kOuts = WR * C * 4, kThreads = WR * 64, kRows = JP * 16;
     constexpr int kPitch = MX ? kOuts / 2 : kOuts * (STAGE32 ? 4 : 2), kHas = kPitch / 16, kMask = kHas >= 8 ? 7 : kHas - 1;
     constexpr int kPieces = MX ? kHas : kOuts * (BF16 ? 2 : 4) / 16, kPer = kOuts / kPieces;   // 16-byte pieces of a stored row; values in one
     constexpr int ES = BF16 ? 2 : 4;
@@ -241,19 +187,19 @@ __device__ inline void store_tile4(const Mx4Product& p, const Channels4<GATED, 4
         __syncthreads();   // the stages, or the outputs before, have been read
 #pragma unroll
         for (int jj = 0; jj < JP; ++jj) {
-            const int lrow = (wt * JP + jj) * 16 + (lane & 15);
+            const int lrow = jj * 16 + (lane & 15);
             char* to = smem + lrow * kPitch;
 #pragma unroll
             for (int run = 0; run < Channels4<GATED, 4>::kRuns; ++run) {
                 float y[8];
                 outputs4<GATED, 4>(ch, acc[j0 + jj], run, y);
-                const int c = wr * C * 4 + run * 32 + (lane >> 4) * 8;   // column in the tile
+                const int c = wave * C * 4 + run * 32 + (lane >> 4) * 8;   // column in the tile
                 if constexpr (MX) {
                     unsigned scale;
                     const unsigned codes = rounded8(y, scale);
                     *reinterpret_cast<unsigned*>(to + ((c >> 5) ^ (lrow & kMask)) * 16 + (lane >> 4) * 4) = codes;
-                    const int row = (wt * TB + j0 + jj) * 16 + (lane & 15), block = (col0 + c) >> 5;
-                    if ((lane >> 4) == 0 && row < t.count && block * 32 < p.outs) p.ys[(t.row0 + row) * p.ldys + block] = (uint8_t)scale;
+                    const int row = (j0 + jj) * 16 + (lane & 15), block = (col0 + c) >> 5;
+                    if ((lane >> 4) == 0 && row < t.count && block * 32 < p.outs) p.ys[((int64_t)t.row0 + row) * p.ldys + block] = (uint8_t)scale;
                 } else if constexpr (STAGE32) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
@@ -270,130 +216,182 @@ __device__ inline void store_tile4(const Mx4Product& p, const Channels4<GATED, 4
 #pragma unroll 4
         for (int u = threadIdx.x; u < kRows * kPieces; u += kThreads) {
             const int lrow = u / kPieces, piece = u % kPieces;
-            const int trow = (lrow / (JP * 16)) * TB * 16 + j0 * 16 + lrow % (JP * 16), col = col0 + piece * kPer;
+            const int trow = j0 * 16 + lrow, col = col0 + piece * kPer;
             if (trow >= t.count || col >= p.outs) continue;
-            const int64_t row = t.row0 + trow;
+            const int64_t row = (int64_t)t.row0 + trow;
             const char* from = smem + lrow * kPitch;
             if constexpr (MX) {
                 store16((char*)p.y + row * p.ldy + (size_t)(col >> 5) * 16, *reinterpret_cast<const u32x4*>(from + (piece ^ (lrow & kMask)) * 16), past);
+                continue;
+            }
+            char* py = (char*)p.y + (row * p.ldy + col) * ES;
+            u32x4 v;
+            if constexpr (STAGE32 && BF16) {
+                const f32x4 a = *reinterpret_cast<const f32x4*>(from + ((2 * piece) ^ (lrow & 7)) * 16);
+                const f32x4 b = *reinterpret_cast<const f32x4*>(from + ((2 * piece + 1) ^ (lrow & 7)) * 16);
+                float y[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+                if (p.res) {
+                    const char* pr = (const char*)p.res + (row * p.ldr + col) * ES;
+                    if (col + 8 <= p.outs) {
+                        float r[8];
+                        Elem<true>::load8(pr, r);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] += r[e];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (col + e < p.outs) y[e] += Elem<true>::load1(pr + e * 2);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = bf16_pair(y[2 * i], y[2 * i + 1]);
             } else {
-                char* py = (char*)p.y + (row * p.ldy + col) * ES;
-                u32x4 v;
-                if constexpr (STAGE32 && BF16) {
-                    const f32x4 a = *reinterpret_cast<const f32x4*>(from + ((2 * piece) ^ (lrow & 7)) * 16);
-                    const f32x4 b = *reinterpret_cast<const f32x4*>(from + ((2 * piece + 1) ^ (lrow & 7)) * 16);
-                    float y[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-                    if (p.res) {
-                        const char* pr = (const char*)p.res + (row * p.ldr + col) * ES;
-                        if (col + 8 <= p.outs) {
-                            float r[8];
-                            Elem<true>::load8(pr, r);
+                v = *reinterpret_cast<const u32x4*>(from + (piece ^ (lrow & 7)) * 16);
+                if (!BF16 && p.res) {
+                    const char* pr = (const char*)p.res + (row * p.ldr + col) * 4;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) y[e] += r[e];
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (col + e < p.outs) y[e] += Elem<true>::load1(pr + e * 2);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = bf16_pair(y[2 * i], y[2 * i + 1]);
-                } else {
-                    v = *reinterpret_cast<const u32x4*>(from + (piece ^ (lrow & 7)) * 16);
-                    if (!BF16 && p.res) {
-                        const char* pr = (const char*)p.res + (row * p.ldr + col) * 4;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (col + e < p.outs) v[e] = __float_as_uint(__uint_as_float(v[e]) + Elem<false>::load1(pr + e * 4));
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < p.outs) v[e] = __float_as_uint(__uint_as_float(v[e]) + Elem<false>::load1(pr + e * 4));
                 }
-                if (col + kPer <= p.outs) {
-                    store16(py, v, past);
-                } else {
+            }
+            if (col + kPer <= p.outs) {
+                store16(py, v, past);
+            } else {
 #pragma unroll
-                    for (int e = 0; e < kPer; ++e)
-                        if (col + e < p.outs) {
-                            if constexpr (BF16) { const unsigned short h = (unsigned short)(v[e / 2] >> (16 * (e & 1))); __builtin_memcpy(py + e * 2, &h, 2); }
-                            else { const unsigned w = v[e]; __builtin_memcpy(py + e * 4, &w, 4); }
-                        }
-                }
+                for (int e = 0; e < kPer; ++e)
+                    if (col + e < p.outs) {
+                        if constexpr (BF16) { const unsigned short h = (unsigned short)(v[e / 2] >> (16 * (e & 1))); __builtin_memcpy(py + e * 2, &h, 2); }
+                        else { const unsigned w = v[e]; __builtin_memcpy(py + e * 4, &w, 4); }
+                    }
             }
         }
     }
 }
 
-template <int WR, int WT, int TB, int NS, int PER_CU, bool GATED, int OUT>
-__global__ __launch_bounds__(WR * WT * 64, PER_CU * WR * WT / 4) void mx4_tile_kernel(Mx4Product p, TileOrder order, const TileHead* head,
-                                                                                      const TileRows* tiles, const unsigned* scales)
+template <int WR, int TB, int NS, int PER_CU, bool GATED, int OUT>
+__global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4Product p, TileBands order)
 {
-    using T = Tile4<WR, WT, TB, NS>;
+    using T = Tile4<WR, TB, NS>;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int wr = wave % WR, wt = wave / WR;
-    int tc, tr, tile, split;
-    if (p.grouped) {   // (tiles past those that there are end here, so that the others are dealt to all XCDs)
-        order.tiles_r = head->tiles;
-        if ((int)blockIdx.x >= order.tiles()) return;
-    }
-    order.at(blockIdx.x, tc, tr, tile, split);
+    const int wave = scalar(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const GroupTiles groups(p, T::kRows);
+    order.tiles_r = groups.all;   // (of experts, those that there are, so that they are dealt to all XCDs)
+    if ((int)blockIdx.x >= order.tiles()) return;
+    int tc, tr;
+    order.at(blockIdx.x, tc, tr);
     tc = scalar(tc);
     tr = scalar(tr);
-    const TileRows t = tile_rows(tiles, tr);
+    const RowTile t = groups.at(p, tr);
     const int g0 = tc * WR, steps = p.steps, halves = steps * 2;
-    const bool own = g0 + wr < p.groups;   // (a wavefront past the last group multiplies zeros)
-    const size_t group = (size_t)t.expert * p.groups + (own ? g0 + wr : 0);
-    const RowTile rt{t.expert, t.count, t.row0};
+    const bool own = g0 + wave < p.groups;   // (a wavefront past the last group multiplies zeros)
+    const size_t group = (size_t)t.expert * p.groups + (own ? g0 + wave : 0);
     const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + group * halves * 4096, own ? (unsigned)halves * 4096 : 0);
     const __amdgpu_buffer_rsrc_t gsr = q8_rsrc(p.ws + group * halves * 64, own ? (unsigned)halves * 256 : 0);
-    const __amdgpu_buffer_rsrc_t xsr = RowBuffers(p, rt).q;
-    const __amdgpu_buffer_rsrc_t ssr = q8_rsrc(scales + (size_t)tr * halves * T::kRows, (unsigned)halves * T::kRows * 4);
+    const RowBuffers from(p, t);
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem;
     constexpr unsigned kNone = 0xc0000000u;   // (and what a lane adds: past the end of weights and scales)
-    // Rows past the tile's last read its first: what comes of them is not stored.  (The scale of a row for an index outside x is NaN.)
+    // Rows past the tile's last read its first: what comes of them is not stored.
+    if (p.index) {
+        for (int i = threadIdx.x; i < T::kRows; i += T::kThreads) *reinterpret_cast<int*>(smem + T::kFromAt + i * 4) = source_of(p, t, i);
+        __syncthreads();
+    }
+    auto source = [&](int row) { return p.index ? *reinterpret_cast<const int*>(smem + T::kFromAt + row * 4) : row < t.count ? row : -1; };
     const int chunk = (lane & 7) ^ (lane >> 3);   // the block of a step that the lane loads, of a row with row & 7 = lane / 8
     unsigned xvoff[T::kXLoads];
 #pragma unroll
     for (int i = 0; i < T::kXLoads; ++i) {
-        const int src = source_of(p, rt, (wave + i * T::kWaves) * 8 + (lane >> 3));
+        const int src = source((wave + i * T::kWaves) * 8 + (lane >> 3));
         xvoff[i] = (unsigned)((src < 0 ? 0 : src) * p.ldq) + chunk * 16;
     }
     const int xsteps = (p.blocks + 7 - chunk) >> 3;   // steps that have it
     const unsigned lane16 = lane * 16, lane4 = lane * 4;
     // load i of step s into the stage at `at`; past the last step nothing is read, so that the count of loads holds
     auto fetch = [&](int i, int s, unsigned at) {
-        if (i < T::kXLoads) {
-            load_to_lds(xsr, s < xsteps ? xvoff[i] + (unsigned)s * 128 : kPast, lds0 + at + (wave + i * T::kWaves) * 1024);
-        } else {
-            const int u = wave + (i - T::kXLoads) * T::kWaves;
-            const bool in = T::kSUnits % T::kWaves == 0 || u < T::kSUnits;
-            load_to_lds4(ssr, (s < steps && in ? (unsigned)s * (T::kRows * 8) + u * 256 : kNone) + lane4, lds0 + (in ? at + T::kXBytes + u * 256 : (unsigned)T::kNowhere));
+        load_to_lds(from.q, s < xsteps ? xvoff[i] + (unsigned)s * 128 : kPast, lds0 + at + (wave + i * T::kWaves) * 1024);
+    };
+    i32x4 w[4][4], x[4];                 // weights of four halves; rows of four blocks
+    unsigned ws[4], xs[2][T::kWords];    // their scales
+    auto weights = [&](int set, int i, int half) {   // load i of a half's
+        const unsigned at = half < halves ? (unsigned)half : kNone >> 12;
+        if (i < 4) w[set][i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wsr, at * 4096 + i * 1024 + lane16, 0, 0));
+        else ws[set] = __builtin_amdgcn_raw_buffer_load_b32(gsr, at * 256 + lane4, 0, 0);
+    };
+    // The scales of 32 halves at a time: a thread takes one half of them, and in turn PASSES times four rows, 16 apart; their words of four blocks
+    // each become for each of those blocks the word of the four rows.
+    constexpr int ROWS = T::kThreads / 32, PASSES = 16 * T::kWords / ROWS;
+    struct Scales {
+        unsigned v[4];
+        bool lost[4];   // (of a row for an index outside x they are NaN)
+    };
+    const uint8_t* scales_of = p.s + (p.index ? 0 : (int64_t)t.row0 * p.lds);
+    auto load_scales = [&](int half, int pass, Scales& s) {
+        const int at = pass * ROWS + (threadIdx.x >> 5), kb = half * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int src = source(((at >> 4) * 4 + j) * 16 + (at & 15));
+            const uint8_t* row = scales_of + (src < 0 ? 0 : src) * p.lds;
+            s.lost[j] = src == -2;
+            // the row's last word, moved down to where its end is, and 1 past that: codes of 0 are multiplied (without branches, so that the
+            // loads of all passes are out together)
+            const int at_kb = kb < p.blocks - 4 ? kb : p.blocks - 4, less = kb - at_kb;
+            unsigned word;
+            __builtin_memcpy(&word, row + at_kb, 4);
+            word = __builtin_amdgcn_alignbyte(0x7f7f7f7fu, word, less & 3);
+            s.v[j] = less < 4 ? word : 0x7f7f7f7fu;
         }
     };
-    i32x4 w[4][4], x[4];            // weights of four halves; rows of four blocks
-    unsigned ws[4], xs[2][TB / 4];  // their scales
-    auto weights = [&](int set, int i, int half) {   // load i of a half's
-        const unsigned from = half < halves ? (unsigned)half : kNone >> 12;
-        if (i < 4) w[set][i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wsr, from * 4096 + i * 1024 + lane16, 0, 0));
-        else ws[set] = __builtin_amdgcn_raw_buffer_load_b32(gsr, from * 256 + lane4, 0, 0);
+    auto put_scales = [&](int half, int pass, Scales& s) {   // `half`: among those in LDS
+        const int at = pass * ROWS + (threadIdx.x >> 5);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s.v[j] = s.lost[j] ? 0xffffffffu : s.v[j];
+        // byte b of word j becomes byte j of word b
+        const unsigned a0 = __builtin_amdgcn_perm(s.v[1], s.v[0], 0x05010400), a1 = __builtin_amdgcn_perm(s.v[1], s.v[0], 0x07030602);
+        const unsigned c0 = __builtin_amdgcn_perm(s.v[3], s.v[2], 0x05010400), c1 = __builtin_amdgcn_perm(s.v[3], s.v[2], 0x07030602);
+        const unsigned out[4] = {(a0 & 0xffffu) | c0 << 16, a0 >> 16 | (c0 & 0xffff0000u), (a1 & 0xffffu) | c1 << 16, a1 >> 16 | (c1 & 0xffff0000u)};
+        if (half < T::kSteps * 2)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) *reinterpret_cast<unsigned*>(smem + T::kSAt + half * T::kHalf + (at >> 4) * 256 + b * 64 + (at & 15) * 4) = out[b];
     };
-    const int xlane = (wt * TB * 16 + (lane & 15)) * 128 + (((lane >> 4) ^ (lane & 7)) << 4), slane = T::kXBytes + wt * TB * 64 + lane * 4;
+    auto deal = [&](int first, int done) {   // those of halves first .., but for the first `done`
+        const int rest = (halves - first + 3) & ~3, end = rest < T::kSteps * 2 ? rest : T::kSteps * 2;
+        for (int h = done; h < end; h += 32)
+#pragma unroll 2
+            for (int i = 0; i < PASSES; ++i) {
+                Scales s;
+                load_scales(first + h + (threadIdx.x & 31), i, s);
+                put_scales(h + (threadIdx.x & 31), i, s);
+            }
+    };
+    const int xlane = (lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) << 4), slane = T::kSAt + lane * 4;
     auto rows = [&](int h, int j, unsigned at) { x[j & 3] = *reinterpret_cast<const i32x4*>(smem + at + (xlane ^ (h * 64)) + j * 2048); };
-    auto row_words = [&](int h, int i, unsigned at) { xs[h][i] = *reinterpret_cast<const unsigned*>(smem + at + slane + h * (T::kRows * 4) + i * 256); };
-    f32x4 acc[TB][4] = {};
+    auto words = [&](int h, int i, unsigned at) { xs[h][i] = *reinterpret_cast<const unsigned*>(smem + slane + at + i * 256); };
+    f32x4 acc[TB][4];
+    // The first scales are asked for before all else: what is asked for later is waited for with them.
+    Scales first[PASSES];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
+    for (int i = 0; i < PASSES; ++i) load_scales(threadIdx.x & 31, i, first[i]);
+    asm volatile("" : : : "memory");
 #pragma unroll
-        for (int i = 0; i < T::kLoads; ++i) fetch(i, s, s * T::kStage);
-        asm volatile("" : : : "memory");   // (the first step's rows are the oldest loads)
-        if (s < 3)
+    for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int i = 0; i < 5; ++i) weights(s, i, s);
-    }
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((NS - 1) * T::kLoads + 15) : "memory");
+        for (int i = 0; i < T::kXLoads; ++i) fetch(i, s, s * T::kXBytes);
+    asm volatile("" : : : "memory");   // (rows first, so that the weights may still be out when they have landed)
+#pragma unroll
+    for (int s = 0; s < 3; ++s)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) weights(s, i, s);
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) put_scales(threadIdx.x & 31, i, first[i]);
+    deal(0, 32);
+#pragma unroll
+    for (int j = 0; j < TB; ++j)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) acc[j][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    asm volatile("s_waitcnt vmcnt(15) lgkmcnt(0)\n\ts_barrier" : : : "memory");
 #pragma unroll
     for (int j = 0; j < 3; ++j) rows(0, j, 0);
 #pragma unroll
-    for (int i = 0; i < TB / 4; ++i) row_words(0, i, 0);
+    for (int i = 0; i < T::kWords; ++i) words(0, i, 0);
     auto multiply = [&](int set, int h, int j) {
         auto four = [&](auto ox) {
             constexpr int OX = decltype(ox)::value;
@@ -407,22 +405,33 @@ __global__ __launch_bounds__(WR * WT * 64, PER_CU * WR * WT / 4) void mx4_tile_k
         else if (j % 4 == 2) four(std::integral_constant<int, 2>{});
         else four(std::integral_constant<int, 3>{});
     };
-    unsigned now = 0;   // the stage that is multiplied
+    unsigned now = 0, scales = 0;   // the stage that is multiplied; the words of its half
+    int left = T::kSteps;           // steps whose scales lie in LDS
     // two steps a turn, for the four sets of weights; past the last step zeros are multiplied
     for (int k = 0; k < halves; k += 4) {
+        if (left == 0) {
+            __syncthreads();   // (the scales have been read)
+            deal(k, 0);
+            __syncthreads();
+            scales = 0;
+            left = T::kSteps;
+#pragma unroll
+            for (int i = 0; i < T::kWords; ++i) words(0, i, 0);
+        }
+        left -= 2;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int h = q & 1;
-            const unsigned then = now + T::kStage == T::kNowhere ? 0 : now + T::kStage;
+            const unsigned then = now + T::kXBytes == T::kSAt ? 0 : now + T::kXBytes;
 #pragma unroll
             for (int j = 0; j < TB; ++j) {
                 // In a step's second half, once all of its rows are read: all wavefronts have read this stage, and the next one has landed.  Younger
-                // than its loads are those of NS - 2 steps and of the weights of four halves.
+                // than its loads are those of NS - 2 steps and of the weights of three halves at least.
                 if (h == 1 && j == TB - 3)
-                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((NS - 2) * T::kLoads + 15) : "memory");
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((NS - 2) * T::kXLoads + 15) : "memory");
                 if (j + 3 < TB) rows(h, j + 3, now);
                 else rows(1 - h, j + 3 - TB, h == 0 ? now : then);
-                if (j >= TB - 3 && j - (TB - 3) < TB / 4) row_words(1 - h, j - (TB - 3), h == 0 ? now : then);
+                if (j >= TB - 3 && j - (TB - 3) < T::kWords) words(1 - h, j - (TB - 3), scales + (q + 1) * T::kHalf);
                 if constexpr (TB == 4) {
                     weights((q + 3) & 3, j, k + q + 3);
                     if (j == 3) weights((q + 3) & 3, 4, k + q + 3);
@@ -431,23 +440,24 @@ __global__ __launch_bounds__(WR * WT * 64, PER_CU * WR * WT / 4) void mx4_tile_k
                 }
                 if (h == 1 && j >= TB - 3)
 #pragma unroll
-                    for (int i = (j - TB + 3) * T::kLoads / 3; i < (j - TB + 4) * T::kLoads / 3; ++i) fetch(i, (k + q) / 2 + NS, now);
+                    for (int i = (j - TB + 3) * T::kXLoads / 3; i < (j - TB + 4) * T::kXLoads / 3; ++i) fetch(i, (k + q) / 2 + NS, now);
                 multiply(q, h, j);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (h == 1) now = then;
         }
+        scales += 4 * T::kHalf;
     }
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // no load into LDS outlives the workgroup
     Channels4<GATED, 4> ch;
-    ch.load(p, t.expert, own ? g0 + wr : p.groups - 1, 0, lane);   // (what a wavefront past the last group has is not stored)
+    ch.load(p, t.expert, own ? g0 + wave : p.groups - 1, 0, lane);   // (what a wavefront past the last group has is not stored)
     constexpr int kOuts = WR * Channels4<GATED, 4>::kRuns * 32;
-    constexpr int JP4 = largest_divisor4(TB, T::kLds / (16 * WT * kOuts * 4)), JP2 = largest_divisor4(TB, T::kLds / (16 * WT * kOuts * 2)),
-                  JPM = largest_divisor4(TB, T::kLds / (16 * WT * kOuts / 2));
-    if constexpr (OUT == NM_MX4) store_tile4<WR, WT, TB, JPM, false, GATED, OUT>(p, ch, acc, smem, wr, wt, lane, g0, t);
-    else if constexpr (OUT == NM_F32) store_tile4<WR, WT, TB, JP4, true, GATED, OUT>(p, ch, acc, smem, wr, wt, lane, g0, t);
-    else if (p.res) store_tile4<WR, WT, TB, JP4, true, GATED, OUT>(p, ch, acc, smem, wr, wt, lane, g0, t);
-    else store_tile4<WR, WT, TB, JP2, false, GATED, OUT>(p, ch, acc, smem, wr, wt, lane, g0, t);
+    constexpr int JP4 = largest_divisor4(TB, T::kLds / (16 * kOuts * 4)), JP2 = largest_divisor4(TB, T::kLds / (16 * kOuts * 2)),
+                  JPM = largest_divisor4(TB, T::kLds / (16 * kOuts / 2));
+    if constexpr (OUT == NM_MX4) store_tile4<WR, TB, JPM, false, GATED, OUT>(p, ch, acc, smem, wave, lane, g0, t);
+    else if constexpr (OUT == NM_F32) store_tile4<WR, TB, JP4, true, GATED, OUT>(p, ch, acc, smem, wave, lane, g0, t);
+    else if (p.res) store_tile4<WR, TB, JP4, true, GATED, OUT>(p, ch, acc, smem, wave, lane, g0, t);
+    else store_tile4<WR, TB, JP2, false, GATED, OUT>(p, ch, acc, smem, wave, lane, g0, t);
 }
 
 // ---------------------------------------------------------------- weights
@@ -548,76 +558,83 @@ int pick_few4(const Mx4Product& p, hipStream_t s)
     return launch_few4<TB, 1, 8, U>(p, s);
 }
 
-// The tile kernels' shapes.
-struct Shape4 {
-    int wr, rows, waves, per_cu;   // per_cu: workgroups that a CU holds (by LDS)
-};
-constexpr Shape4 kShapes4[] = {{4, 256, 8, 1},    // 256 packed channels x 256 rows
-                               {4, 128, 4, 2},
-                               {4, 64, 4, 2}};
+constexpr int kFewRows4 = 64;
 
-template <int SHAPE, int WT, int TB, int NS, bool GATED, int OUT>
-int launch_tile4(const Mx4Product& p, const Mx4Plan& pl, char* workspace, hipStream_t s)
+// What runs a call: a tile shape, or the few-row kernels (-1).
+struct Mx4Plan {
+    int shape = -1;
+    int64_t tiles = 0;   // of rows, at most
+};
+
+// The tile kernels' shapes.  More rows a workgroup read weights less often and keep the matrix units busier; fewer make more workgroups, and
+// leave less of a group's last tile empty.
+struct Shape4 {
+    int wr, rows, waves, per_cu;      // per_cu: workgroups that a CU holds (by registers)
+    float fixed, alone, shared;       // us: of a tile; of a step with one workgroup a CU, with two
+};
+constexpr Shape4 kShapes4[] = {{4, 128, 4, 2, 5.5f, 0.70f, 1.80f},    // 256 packed channels x 128 rows
+                               {4, 64, 4, 2, 5.0f, 0.49f, 1.25f}};
+
+template <int SHAPE, int TB, int NS, bool GATED, int OUT>
+int launch_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 {
-    constexpr int WR = kShapes4[SHAPE].wr;
-    using T = Tile4<WR, WT, TB, NS>;
+    constexpr int WR = kShapes4[SHAPE].wr, PER_CU = kShapes4[SHAPE].per_cu;
+    using T = Tile4<WR, TB, NS>;
     static_assert(T::kWaves == kShapes4[SHAPE].waves && T::kRows == kShapes4[SHAPE].rows, "kShapes4 describes the kernels");
-    TileOrder o;
-    o.splits = 1;
-    o.tiles_c = (p.groups + WR - 1) / WR;
-    o.tiles_r = (int)pl.tiles;
-    const int64_t grid = pl.tiles * o.tiles_c, parts = T::kRows / 64;
-    if (grid > 0x7fffffff || pl.tiles * parts > 0x7fffffff) {
+    const TileBands o{(p.groups + WR - 1) / WR, (int)pl.tiles, 8};
+    const int64_t grid = pl.tiles * o.tiles_c;
+    if (grid > 0x7fffffff) {
         set_error("%lld tiles: too many", (long long)grid);
         return NM_ERR_SHAPE;
     }
-    TileHead* head = (TileHead*)workspace;
-    TileRows* tiles = (TileRows*)(head + 1);
-    unsigned* scales = (unsigned*)(workspace + pl.tile_bytes);
-    hipLaunchKernelGGL(mx4_scales_kernel, dim3((unsigned)(pl.tiles * parts), (unsigned)(p.steps < 32 ? (p.steps + 1) / 2 : 16)), dim3(256), 0, s, p, T::kRows, head, tiles, scales);
-    NM_HIP_CHECK(hipGetLastError());
     static unsigned long long done = 0;
-    const int rc = allow_lds((const void*)mx4_tile_kernel<WR, WT, TB, NS, kShapes4[SHAPE].per_cu, GATED, OUT>, T::kLds, &done);
+    const int rc = allow_lds((const void*)mx4_tile_kernel<WR, TB, NS, PER_CU, GATED, OUT>, T::kLds, &done);
     if (rc != NM_OK) return rc;
-    hipLaunchKernelGGL((mx4_tile_kernel<WR, WT, TB, NS, kShapes4[SHAPE].per_cu, GATED, OUT>), dim3((unsigned)grid), dim3(T::kWaves * 64), T::kLds, s, p, o,
-                       (const TileHead*)head, (const TileRows*)tiles, (const unsigned*)scales);
+    hipLaunchKernelGGL((mx4_tile_kernel<WR, TB, NS, PER_CU, GATED, OUT>), dim3((unsigned)grid), dim3(T::kWaves * 64), T::kLds, s, p, o);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }
 
 template <bool GATED, int OUT>
-int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, char* workspace, hipStream_t s)
+int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 {
-    switch (pl.shape) {
-    case 0: return launch_tile4<0, 2, 8, 3, GATED, OUT>(p, pl, workspace, s);
-    case 1: return launch_tile4<1, 1, 8, 3, GATED, OUT>(p, pl, workspace, s);
-    default: return launch_tile4<2, 1, 4, 4, GATED, OUT>(p, pl, workspace, s);
-    }
+    if (pl.shape == 0) return launch_tile4<0, 8, 3, GATED, OUT>(p, pl, s);
+    return launch_tile4<1, 4, 4, GATED, OUT>(p, pl, s);
 }
 
 }  // namespace
 
-Mx4Plan mx4_plan(const Mx4Product& p)
+// The shape with the least estimated time: rounds of workgroups over 256 CUs, two a CU.  Groups leave half a tile empty each.
+// us, 128 rows and 64: 512 x 4096 -> 4096 17.4 and 13.3, 2048 x 4096 -> 8192 37 and 50, 8192 x 4096 -> 16384 270 and 330, 60 experts
+// of 12004 x 1440 -> 1111 37 and 35, 64 of 32768 x 2048 -> 2 x 1024 107 and 123.
+static Mx4Plan mx4_plan(const Mx4Product& p)
 {
     Mx4Plan pl;
     const int64_t each = p.grouped ? (p.rows + p.experts - 1) / p.experts : p.rows;
-    if (each <= NM_MX4_FEW_ROWS) return pl;
-    pl.shape = each >= 256 ? 0 : 2;
-    if (pl.shape < 0) return pl;
-    const int per = kShapes4[pl.shape].rows;
-    pl.tiles = tiles_of(p, per);
-    pl.tile_bytes = (sizeof(TileHead) + (size_t)pl.tiles * sizeof(TileRows) + 255) / 256 * 256;
-    pl.scale_bytes = (size_t)pl.tiles * per * p.steps * 8;
+    if (each <= kFewRows4 || p.blocks < 4) return pl;   // (the tile kernels read scales by fours)
+    float least = 1e30f;
+    for (int sh = 0; sh < (int)(sizeof(kShapes4) / sizeof(Shape4)); ++sh) {
+        const Shape4& k = kShapes4[sh];
+        const int64_t groups = p.grouped ? p.experts : 0;
+        const int64_t tiles = (groups ? p.rows / k.rows + (groups + 1) / 2 : (p.rows + k.rows - 1) / k.rows) * ((p.groups + k.wr - 1) / k.wr);
+        const int64_t rounds = tiles / 512, rest = tiles % 512;
+        const float us = rounds * (k.fixed + p.steps * k.shared) + (rest ? k.fixed + p.steps * (rest > 256 ? k.shared : k.alone) : 0.0f);
+        if (us < least) {
+            least = us;
+            pl.shape = sh;
+        }
+    }
+    pl.tiles = tiles_of(p, kShapes4[pl.shape].rows);
     return pl;
 }
 
-int run_mx4_product(const Mx4Product& p, const Mx4Plan& pl, void* workspace, hipStream_t s)
+int run_mx4_product(const Mx4Product& p, hipStream_t s)
 {
+    const Mx4Plan pl = mx4_plan(p);
     if (pl.shape >= 0) {
-        char* ws = (char*)workspace;
-        if (p.out == NM_MX4) return p.gated ? pick_tile4<true, NM_MX4>(p, pl, ws, s) : pick_tile4<false, NM_MX4>(p, pl, ws, s);
-        if (p.out == NM_BF16) return p.gated ? pick_tile4<true, NM_BF16>(p, pl, ws, s) : pick_tile4<false, NM_BF16>(p, pl, ws, s);
-        return p.gated ? pick_tile4<true, NM_F32>(p, pl, ws, s) : pick_tile4<false, NM_F32>(p, pl, ws, s);
+        if (p.out == NM_MX4) return p.gated ? pick_tile4<true, NM_MX4>(p, pl, s) : pick_tile4<false, NM_MX4>(p, pl, s);
+        if (p.out == NM_BF16) return p.gated ? pick_tile4<true, NM_BF16>(p, pl, s) : pick_tile4<false, NM_BF16>(p, pl, s);
+        return p.gated ? pick_tile4<true, NM_F32>(p, pl, s) : pick_tile4<false, NM_F32>(p, pl, s);
     }
     const int64_t each = p.grouped ? (p.rows + p.experts - 1) / p.experts : p.rows;
     if (each <= 16) return pick_few4<1>(p, s);
