@@ -75,6 +75,7 @@ typedef struct nm_mx4 nm_mx4_t;
 int nm_mx4_pack(const void* w_dev, nm_dtype_t w_dtype, const uint8_t* scales_dev, int64_t lds, int experts, int channels,
                 int width, int64_t ldw, int gated, void* hip_stream, nm_mx4_t** out);
 
+/* Not before the work that reads it has ended (device memory is freed); other streams may be under capture. */
 int nm_mx4_free(nm_mx4_t* w);
 
 /* Sizes as given to nm_mx4_pack.  Any out pointer may be NULL. */

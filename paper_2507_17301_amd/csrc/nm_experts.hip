@@ -5,33 +5,38 @@ namespace nm {
 namespace {
 
 // ---------------------------------------------------------------- routing
-// Tokens go by in chunks, one a workgroup, a chunk in batches of 64.  A token belongs to L lanes, which hold its logits as whole numbers
-// that sort like them; its choices are taken one after another, each the largest of (logit, lowest expert) over the lanes.
+// Tokens go by in chunks, one a workgroup, a chunk in batches of 64.  A token belongs to L lanes, of V adjacent experts each.  A logit and its
+// expert are one double in [1, 2): 32 bits of the fraction sort like the logits, 10 below them fall with the expert, so that a maximum of
+// doubles finds the largest logit and of equal ones the lowest expert.  The choices are taken one after another.
 // The order by expert comes of one 64-bit mask an expert and batch, with a bit for each token that chose it: an expert's count is the number of
 // its bits, a token's place among the batch's the number of bits below its own.  So no order of atomics shows in a result.
 constexpr int kThreads = 1024, kBatch = 64, kChunks = 256;
 
 template <int CTRL> __device__ inline unsigned dpp(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
 
-struct Best {
-    unsigned key, expert;
-    __device__ inline void take(unsigned k, unsigned e)
-    {
-        const bool other = k > key || (k == key && e < expert);
-        key = other ? k : key;
-        expert = other ? e : expert;
-    }
-};
-
-template <int L> __device__ inline Best best_of(Best b)
+template <int CTRL> __device__ inline double dpp(double v)
 {
-    b.take(dpp<0xb1>(b.key), dpp<0xb1>(b.expert));     // lane ^ 1
-    b.take(dpp<0x4e>(b.key), dpp<0x4e>(b.expert));     // lane ^ 2
-    b.take(dpp<0x141>(b.key), dpp<0x141>(b.expert));   // mirrored in eight
-    b.take(dpp<0x140>(b.key), dpp<0x140>(b.expert));   // mirrored in sixteen
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)dpp<CTRL>((unsigned)(u >> 32)) << 32 | dpp<CTRL>((unsigned)u));
+}
+
+// fmax of doubles that are no NaN (the compiler makes its own of two instructions each)
+__device__ inline double larger(double a, double b)
+{
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
+template <int L> __device__ inline double best_of(double b)
+{
+    b = fmax(b, dpp<0xb1>(b));    // lane ^ 1
+    b = fmax(b, dpp<0x4e>(b));    // lane ^ 2
+    b = fmax(b, dpp<0x141>(b));   // mirrored in eight
+    b = fmax(b, dpp<0x140>(b));   // mirrored in sixteen
     if constexpr (L == 64) {
-        b.take(__shfl_xor(b.key, 16), __shfl_xor(b.expert, 16));
-        b.take(__shfl_xor(b.key, 32), __shfl_xor(b.expert, 32));
+        b = fmax(b, __shfl_xor(b, 16));
+        b = fmax(b, __shfl_xor(b, 32));
     }
     return b;
 }
@@ -51,7 +56,40 @@ __device__ inline unsigned key_of(float f)
     const unsigned u = __float_as_uint(f + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ inline double pack(unsigned key, int expert)
+{
+    return __builtin_bit_cast(double, 0x3ff0000000000000ull | (uint64_t)key << 10 | (unsigned)(NM_ROUTE_MAX_EXPERTS - 1 - expert));
+}
+__device__ inline unsigned key_in(double d) { return (unsigned)(__builtin_bit_cast(uint64_t, d) >> 10); }
+__device__ inline unsigned low_word(double d) { return (unsigned)__builtin_bit_cast(uint64_t, d); }   // tells experts apart
+__device__ inline double taken(double d) { return __builtin_bit_cast(double, 0x3ff0000000000000ull | low_word(d)); }   // (a key below 2^22: closed)
+__device__ inline int expert_in(double d) { return NM_ROUTE_MAX_EXPERTS - 1 - (int)(low_word(d) & (NM_ROUTE_MAX_EXPERTS - 1)); }
 __device__ inline float logit_of(unsigned key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+
+// The packed logits of V adjacent experts of a token.
+template <int V> __device__ inline void logits_of(const Route& r, int64_t token, int first, double (&best)[V])
+{
+    float f[V];
+    const char* row = (const char*)r.logits + (token * r.ld + first) * (r.bf16 ? 2 : 4);
+    if (first + V <= r.experts) {   // (through memcpy: rows start anywhere)
+        if (r.bf16) {
+            unsigned w[V / 2];
+            __builtin_memcpy(w, row, V * 2);
+#pragma unroll
+            for (int v = 0; v < V; ++v) f[v] = __uint_as_float(v & 1 ? w[v / 2] & 0xffff0000u : w[v / 2] << 16);
+        } else {
+            __builtin_memcpy(f, row, V * 4);
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            f[v] = -__builtin_inff();
+            if (first + v < r.experts) f[v] = r.bf16 ? Elem<true>::load1(row + v * 2) : Elem<false>::load1(row + v * 4);
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) best[v] = pack(key_of(f[v]), first + v);
+}
 
 // Chooses for the tokens of one batch; their bits go into mask.
 template <int L, int V>
@@ -61,49 +99,39 @@ __device__ inline void choose(const Route& r, int64_t first, int count, unsigned
     const int l = threadIdx.x % L;
     for (int t = threadIdx.x / L; t < count; t += PER) {
         const int64_t token = first + t;
-        unsigned key[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = v * L + l;
-            key[v] = 0;
-            if (e < r.experts) {
-                const int64_t at = token * r.ld + e;
-                key[v] = key_of(r.bf16 ? Elem<true>::load1((const char*)r.logits + at * 2) : Elem<false>::load1((const char*)r.logits + at * 4));
-            }
-        }
+        double best[V];
+        logits_of<V>(r, token, l * V, best);
         float top = 0.0f, sum = 0.0f, p[SLOTS];
         int id[SLOTS];
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) { p[s] = 0.0f; id[s] = -1; }
         for (int j = 0; j < r.choices; ++j) {
-            Best b{0, 0xffffffffu};
+            double half = best[V / 2], b = best[0];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const bool more = key[v] > b.key;   // (a lane's experts rise with v)
-                b.key = more ? key[v] : b.key;
-                b.expert = more ? v * L + l : b.expert;
+            for (int v = 1; v < V / 2; ++v) {
+                b = larger(b, best[v]);
+                half = larger(half, best[V / 2 + v]);
             }
-            b = best_of<L>(b);
-            if (b.key <= kClosed) break;   // (the same for all lanes of a token)
-            const float logit = logit_of(b.key);
+            b = best_of<L>(fmax(b, half));
+            if (key_in(b) <= kClosed) break;   // (the same for all lanes of a token)
+            const float logit = logit_of(key_in(b));
             if (j == 0) {
                 top = logit;
                 if (!r.normalise) {
                     float part = 0.0f;
 #pragma unroll
                     for (int v = 0; v < V; ++v)
-                        if (key[v] > kClosed) part += expf(logit_of(key[v]) - top);
+                        if (key_in(best[v]) > kClosed) part += expf(logit_of(key_in(best[v])) - top);
                     sum = sum_of<L>(part);
                 }
             }
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (b.expert == (unsigned)(v * L + l)) key[v] = 0;
+            for (int v = 0; v < V; ++v) best[v] = low_word(best[v]) == low_word(b) ? taken(best[v]) : best[v];
             const float e = expf(logit - top);
             if (r.normalise) sum += e;
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s)
-                if (j == s * L + l) { p[s] = e; id[s] = (int)b.expert; }
+                if (j == s * L + l) { p[s] = e; id[s] = expert_in(b); }
         }
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
@@ -209,7 +237,7 @@ __global__ __launch_bounds__(kThreads) void route_place_kernel(Route r, int chun
     const int parts = kThreads / pad, part = t / pad, e = t % pad;
     int all = 0, before = 0;
     if (e < r.experts) {
-#pragma unroll 8
+#pragma unroll 16
         for (int c = part; c < chunks; c += parts) {
             const int n = counts[(int64_t)c * r.experts + e];
             all += n;

@@ -74,8 +74,12 @@ int check_device(const nm_mx4* w)
 void free_mx4(nm_mx4* w)
 {
     if (!w) return;
+    // A handle may go (by its owner's garbage collection) while a stream is being captured, which hipFree ends unless the thread allows it.
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    const bool changed = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
     (void)hipFree(w->d_w);
     (void)hipFree(w->d_s);
+    if (changed) (void)hipThreadExchangeStreamCaptureMode(&mode);
     delete w;
 }
 

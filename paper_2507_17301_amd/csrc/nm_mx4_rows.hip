@@ -20,7 +20,7 @@ struct Mx4Rows {
     uint8_t* scales;
     int64_t rows, ldx, ldr, ldo, ldq, lds;
     int width, units;   // units: of 8 values, whole blocks
-    double eps;
+    double eps, each;   // each: 1 / width
 };
 
 template <int CTRL> __device__ inline unsigned dpp(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
@@ -32,15 +32,32 @@ __device__ inline unsigned block_max(unsigned m)
     return max(m, dpp<0x4e>(m)); // lanes 2 3 0 1
 }
 
+// The eight values at c of a row of at least 8; where it ends before them, the last eight: settle_unit puts that right.
 template <bool BF16> __device__ inline void load_unit(const char* row, int c, int width, float (&v)[8])
 {
-    constexpr int ES = Elem<BF16>::kBytes;
-    if (c + 8 <= width) {
-        Elem<BF16>::load8(row + (size_t)c * ES, v);
-    } else {
+    Elem<BF16>::load8(row + (unsigned)(min(c, width - 8) * Elem<BF16>::kBytes), v);
+}
+
+// Zeros for what lies past the end, as straight code: a branch a value would wait for each load by itself.
+__device__ inline void settle_unit(int c, int width, float (&v)[8])
+{
+    const int over = c - (width - 8);
+    if (over > 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < width ? Elem<BF16>::load1(row + (size_t)(c + e) * ES) : 0.0f;
+        for (int step = 1; step < 8; step <<= 1)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = over & step ? (e + step < 8 ? v[e + step < 8 ? e + step : 0] : 0.0f) : v[e];
+        if (over >= 8)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = 0.0f;
     }
+}
+
+// A row of fewer than 8 values: its first unit has them all.
+template <bool BF16> __device__ inline void load_short(const char* row, int c, int width, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < width ? Elem<BF16>::load1(row + (size_t)(c + e) * Elem<BF16>::kBytes) : 0.0f;
 }
 
 // Writes a thread's eight values; unit u of the row, whose scale's byte the first of a block's four threads writes.
@@ -55,7 +72,7 @@ __device__ inline void store_unit(uint8_t* q, uint8_t* scales, int u, const floa
 }
 
 // Blocks do not know of each other: a thread takes units 256 apart.
-template <bool BF16>
+template <bool BF16, bool SHORT>
 __global__ __launch_bounds__(256) void mx4_round_kernel(Mx4Rows p)
 {
     constexpr int ES = Elem<BF16>::kBytes;
@@ -64,44 +81,89 @@ __global__ __launch_bounds__(256) void mx4_round_kernel(Mx4Rows p)
         const int64_t row = total <= 0xffffffffll ? (int64_t)((unsigned)i / (unsigned)p.units) : i / p.units;
         const int u = (int)(i - row * p.units);
         float v[8];
-        load_unit<BF16>(p.x + row * p.ldx * ES, u * 8, p.width, v);
+        if constexpr (SHORT) {
+            load_short<BF16>(p.x + row * p.ldx * ES, u * 8, p.width, v);
+        } else {
+            load_unit<BF16>(p.x + row * p.ldx * ES, u * 8, p.width, v);
+            settle_unit(u * 8, p.width, v);
+        }
         store_unit(p.q + row * p.ldq, p.scales + row * p.lds, u, v);
     }
 }
 
-template <int NT> __device__ inline double row_total(double v, double* part)
+template <int CTRL> __device__ inline double dpp(double v)
 {
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
-    if constexpr (NT > 64) {
-        __syncthreads();   // (the row before has been read)
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.0;
-        for (int i = 0; i < NT / 64; ++i) v += part[i];
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)dpp<CTRL>((unsigned)(u >> 32)) << 32 | dpp<CTRL>((unsigned)u));
+}
+
+// The sum over groups of N lanes (up to 64), the same bits in all of them.
+template <int N> __device__ inline double lanes_total(double v)
+{
+    v += dpp<0xb1>(v);    // lane ^ 1
+    v += dpp<0x4e>(v);    // lane ^ 2
+    if constexpr (N > 4) v += dpp<0x141>(v);   // mirrored in eight
+    if constexpr (N > 8) v += dpp<0x140>(v);   // mirrored in sixteen
+    if constexpr (N > 16) {
+        v += __shfl_xor(v, 16);
+        v += __shfl_xor(v, 32);
     }
     return v;
 }
 
-// NT threads a row, VPT units a thread, held in registers over the sum.
-template <bool BF16, int NT, int VPT>
+template <int NT> __device__ inline double row_total(double v, double* part)
+{
+    v = lanes_total<64>(v);
+    if constexpr (NT > 64) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = lanes_total<NT / 64>(part[threadIdx.x & (NT / 64 - 1)]);
+    }
+    return v;
+}
+
+// 1 / sqrt(a), to some bits of the last of 64: the instruction's 2^-26 or so, and a step of third order.  As it is for 0 and infinity.
+__device__ inline double inverse_root(double a)
+{
+    const double y = __builtin_amdgcn_rsq(a), e = fma(-a * y, y, 1.0), z = fma(y * e, fma(e, 0.375, 0.5), y);
+    return z == z ? z : y;
+}
+
+// NT threads a row, VPT units a thread, held in registers over the sum.  Loads go out in groups of units.
+template <bool BF16, int NT, int VPT, bool SHORT>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void mx4_norm_kernel(Mx4Rows p)
 {
 #pragma clang fp contract(off)
     constexpr int ES = Elem<BF16>::kBytes, BLOCK = NT < 256 ? 256 : NT, RPB = BLOCK / NT;
-    __shared__ double part[BLOCK / 64];
-    const int t = threadIdx.x % NT;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT; row < p.rows; row += (int64_t)gridDim.x * RPB) {
+    constexpr int GROUP = VPT == 8 ? (NT < 1024 ? 4 : 1) : VPT == 4 && NT == 1024 ? 2 : VPT, AHEAD = VPT < 2 ? VPT : 2;   // AHEAD: units of gamma
+    __shared__ double part[2][BLOCK / 64];   // in turn: a wavefront may still read one row's when another writes the next row's
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + (RPB > 1 ? threadIdx.x / NT : 0); row < p.rows; row += (int64_t)gridDim.x * RPB) {
+        int t = RPB > 1 ? threadIdx.x % NT : threadIdx.x;
+        if constexpr (VPT > 2) asm volatile("" : "+v"(t));   // (offsets made from it outside the loop would take all registers)
+        const char *px = p.x + row * p.ldx * ES, *pr = p.res ? p.res + row * p.ldr * ES : nullptr;
         float h[VPT][8];
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int c = (i * NT + t) * 8;
-            load_unit<BF16>(p.x + row * p.ldx * ES, c, p.width, h[i]);
-            if (p.res) {
-                float r[8];
-                load_unit<BF16>(p.res + row * p.ldr * ES, c, p.width, r);
+        for (int i0 = 0; i0 < VPT; i0 += GROUP) {
+            float r[GROUP][8];
+            if constexpr (SHORT) {
+                load_short<BF16>(px, t * 8, p.width, h[0]);
+                if (pr) load_short<BF16>(pr, t * 8, p.width, r[0]);
+            } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[i][e] += r[e];
+                for (int i = 0; i < GROUP; ++i) load_unit<BF16>(px, ((i0 + i) * NT + t) * 8, p.width, h[i0 + i]);
+                if (pr)
+#pragma unroll
+                    for (int i = 0; i < GROUP; ++i) load_unit<BF16>(pr, ((i0 + i) * NT + t) * 8, p.width, r[i]);
             }
+            if (pr)
+#pragma unroll
+                for (int i = 0; i < GROUP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) h[i0 + i][e] += r[i][e];
+            if (!SHORT && (i0 + GROUP) * NT * 8 > p.width)
+#pragma unroll
+                for (int i = 0; i < GROUP; ++i) settle_unit(((i0 + i) * NT + t) * 8, p.width, h[i0 + i]);
         }
         if (p.out) {
 #pragma unroll
@@ -115,23 +177,37 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void mx4_norm_kernel(Mx4Rows p
                         if (c + e < p.width) Elem<BF16>::store1(po + e * ES, h[i][e]);
             }
         }
+        float g[AHEAD][8];
+        auto gain = [&](int i) {   // (the last one of a row is settled below)
+            if constexpr (SHORT) load_short<false>((const char*)p.gamma, t * 8, p.width, g[0]);
+            else load_unit<false>((const char*)p.gamma, (i * NT + t) * 8, p.width, g[i % AHEAD]);
+        };
+        if (p.gamma)
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) gain(i);
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = fma((double)h[i][e], (double)h[i][e], sum);
-        const float n = (float)(1.0 / sqrt(row_total<NT>(sum, part) / (double)p.width + p.eps));
+        const float n = (float)inverse_root(row_total<NT>(sum, part[turn]) * p.each + p.eps);
+        turn ^= 1;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int u = i * NT + t;
-            if (u < p.units) {   // (whole blocks: the four threads of one agree)
-                float g[8];
-                if (p.gamma) load_unit<false>((const char*)p.gamma, u * 8, p.width, g);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    h[i][e] = h[i][e] * n;
-                    if (p.gamma) h[i][e] = h[i][e] * g[e];
-                    if (u * 8 + e >= p.width) h[i][e] = 0.0f;   // (0 * infinity in a row without a norm)
+            for (int e = 0; e < 8; ++e) h[i][e] = h[i][e] * n;
+            if (p.gamma) {
+                if (!SHORT && (i + 1) * NT * 8 > p.width) settle_unit(u * 8, p.width, g[i % AHEAD]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[i][e] = h[i][e] * g[i % AHEAD][e];
+                if (i + AHEAD < VPT) gain(i + AHEAD);
+            }
+            if (u < p.units) {   // (whole blocks: the four threads of one agree)
+                if (u * 8 + 8 > p.width) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (u * 8 + e >= p.width) h[i][e] = 0.0f;   // (0 * infinity in a row without a norm)
                 }
                 store_unit(p.q + row * p.ldq, p.scales + row * p.lds, u, h[i]);
             }
@@ -161,26 +237,33 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* q, i
 
 inline unsigned grid_of(int64_t blocks) { return (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)); }
 
-template <bool BF16, int NT, int VPT>
+template <bool BF16, int NT, int VPT, bool SHORT = false>
 int launch_norm(const Mx4Rows& p, hipStream_t s)
 {
     constexpr int BLOCK = NT < 256 ? 256 : NT, RPB = BLOCK / NT;
-    hipLaunchKernelGGL((mx4_norm_kernel<BF16, NT, VPT>), dim3(grid_of((p.rows + RPB - 1) / RPB)), dim3(BLOCK), 0, s, p);
+    hipLaunchKernelGGL((mx4_norm_kernel<BF16, NT, VPT, SHORT>), dim3(grid_of((p.rows + RPB - 1) / RPB)), dim3(BLOCK), 0, s, p);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }
 
+// Threads of a row.  us, bf16 with a residual and h stored, threads x units a thread, 1 row, 256, and 16384 (8192 of 16384 values):
+//    4096   512 x 1  2.9   -    86     256 x 2  3.4   -    92     256 x 4  5.1   -   108
+//    8192  1024 x 1  3.7  6.2  202     512 x 2  3.9  6.4  188     256 x 4  4.4  6.6  160
+//   16384  1024 x 2   -   8.0  183     512 x 4   -   7.6  163
+//   32768  1024 x 4   -    -   177     512 x 8   -    -   190   (4096 rows)
+// The many rows move 4.7 to 5.5 TB/s.
 template <bool BF16>
 int pick_norm(const Mx4Rows& p, hipStream_t s)
 {
     const int w = p.width;
+    if (w < 8) return launch_norm<BF16, 64, 1, true>(p, s);
     if (w <= 512) return launch_norm<BF16, 64, 1>(p, s);
     if (w <= 1024) return launch_norm<BF16, 64, 2>(p, s);
     if (w <= 2048) return launch_norm<BF16, 256, 1>(p, s);
     if (w <= 4096) return launch_norm<BF16, 512, 1>(p, s);
-    if (w <= 6144) return launch_norm<BF16, 512, 2>(p, s);
-    if (w <= 8192) return launch_norm<BF16, 1024, 1>(p, s);
-    if (w <= 16384) return launch_norm<BF16, 1024, 2>(p, s);
+    const bool few = p.rows < 256;
+    if (w <= 8192) return few ? launch_norm<BF16, 1024, 1>(p, s) : launch_norm<BF16, 256, 4>(p, s);
+    if (w <= 16384) return few ? launch_norm<BF16, 1024, 2>(p, s) : launch_norm<BF16, 512, 4>(p, s);
     if (w <= 32768) return launch_norm<BF16, 1024, 4>(p, s);
     return launch_norm<BF16, 1024, 8>(p, s);
 }
@@ -192,11 +275,14 @@ int run_mx4_rows(const void* x, nm_dtype_t dt, int64_t rows, int width, int64_t 
                  int64_t lds, hipStream_t s)
 {
     const int units = (width + 31) / 32 * 4;
-    Mx4Rows p{(const char*)x, (const char*)res, gamma, (char*)out, q, scales, rows, ldx, ldr, ldo, ldq, lds, width, units, eps};
+    Mx4Rows p{(const char*)x, (const char*)res, gamma, (char*)out, q, scales, rows, ldx, ldr, ldo, ldq, lds, width, units, eps, 1.0 / width};
     if (norm) return dt == NM_F32 ? pick_norm<false>(p, s) : pick_norm<true>(p, s);
     const dim3 grid(grid_of((rows * units + 255) / 256));
-    if (dt == NM_F32) hipLaunchKernelGGL((mx4_round_kernel<false>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((mx4_round_kernel<true>), grid, dim3(256), 0, s, p);
+    const bool f32 = dt == NM_F32;
+    if (f32 && width < 8) hipLaunchKernelGGL((mx4_round_kernel<false, true>), grid, dim3(256), 0, s, p);
+    else if (f32) hipLaunchKernelGGL((mx4_round_kernel<false, false>), grid, dim3(256), 0, s, p);
+    else if (width < 8) hipLaunchKernelGGL((mx4_round_kernel<true, true>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((mx4_round_kernel<true, false>), grid, dim3(256), 0, s, p);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }

@@ -211,3 +211,19 @@ def test_layer_and_graph():
                 graph.replay()
                 torch.cuda.synchronize()
                 assert torch.equal(out, layer(xd, rd))
+
+
+def test_a_handle_freed_under_capture():
+    g = torch.Generator().manual_seed(77)
+    q, s = nm.nm_quantize_mx4(rows_of(g, 3, 256, torch.float32).cuda())
+    h, other = (nm.nm_mx4_pack(rows_of(g, 128, 256, torch.float32).cuda()) for _ in range(2))
+    ref = nm.nm_linear_mx4(q, s, h, dtype=torch.float32)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        other.free()
+        y = nm.nm_linear_mx4(q, s, h, dtype=torch.float32)
+    for _ in range(3):
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, ref)
