@@ -13,17 +13,17 @@ namespace nm {
 namespace {
 
 // ---------------------------------------------------------------- few rows
-// Tiles of up to 16 * TB rows.  A workgroup owns RB blocks of 16 packed channels; its NW wavefronts take the steps of 256 k in turn, U of them
-// in flight each, and add their sums through LDS at the end, in the order of the wavefronts.  Weights go from memory into registers: a
+// Tiles of up to 16 * TB rows.  A workgroup owns RB blocks of 16 packed channels; its NW wavefronts take the steps of 256 k in turn, and add
+// their sums through LDS at the end, in the order of the wavefronts.  Weights go from memory into registers: a
 // weight is used once, there is nothing to share.  Rows of x go through LDS, a part of it for each wavefront, so that 8 lanes read the 128
 // adjacent bytes of a row.
-template <int TB, int RB, int NW, int U> constexpr int few4_lds()
+template <int TB, int RB, int NW> constexpr int few4_lds()
 {
-    const int rows = NW * U * TB * 2048, sums = NW * RB * TB * 1024;
+    const int rows = NW * TB * 2048, sums = NW * RB * TB * 1024;
     return rows > sums ? rows : sums;
 }
 
-template <int TB, int RB, int NW, int U>
+template <int TB, int RB, int NW>
 __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int parts)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -36,7 +36,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
     const __amdgpu_buffer_rsrc_t ssr = q8_rsrc(p.ws + group * p.steps * 128, (unsigned)p.steps * 512);
     const RowBuffers from(p, t);
     const unsigned woff = (b0 & 3) * 1024 + lane * 16, soff = lane * 4;
-    const unsigned mine = wave * (U * TB * 2048), lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem + mine;
+    const unsigned mine = wave * (TB * 2048), lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem + mine;
     const unsigned at = mine + (lane & 15) * 128;
     unsigned qoff[TB][2];   // 8 rows an instruction, block c of a row at c ^ (row & 7)
     int source[TB];
@@ -51,53 +51,44 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
         source[i] = source_of(p, t, i * 16 + (lane & 15));
     }
     f32x4 acc[RB][TB] = {};
-    for (int k0 = wave; k0 < p.steps; k0 += NW * U) {
-        i32x4 wf[U][2][RB];
-        unsigned wsc[U][2], xsc[U][TB];
+    for (int k = wave; k < p.steps; k += NW) {
+        i32x4 wf[2][RB];
+        unsigned wsc[2], xsc[TB];
+        const bool row_in = k * 8 + chunk < p.blocks;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int k = k0 + u * NW;
-            const bool in = k < p.steps;   // past the last step nothing is read and zeros are multiplied
-            const bool row_in = k * 8 + chunk < p.blocks;
-#pragma unroll
-            for (int i = 0; i < TB; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    load_to_lds(from.q, row_in && qoff[i][h] != kPast ? qoff[i][h] + k * 128 : kPast, lds0 + u * TB * 2048 + i * 2048 + h * 1024);
+        for (int i = 0; i < TB; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
+                load_to_lds(from.q, row_in && qoff[i][h] != kPast ? qoff[i][h] + k * 128 : kPast, lds0 + i * 2048 + h * 1024);
 #pragma unroll
-                for (int i = 0; i < RB; ++i)
-                    wf[u][h][i] = __builtin_bit_cast(
-                        i32x4, __builtin_amdgcn_raw_buffer_load_b128(wsr, in ? woff + i * 1024 + (k * 2 + h) * 4096 : kPast, 0, 2));
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) wsc[u][h] = __builtin_amdgcn_raw_buffer_load_b32(ssr, in ? soff + (k * 2 + h) * 256 : kPast, 0, 0);
+            for (int i = 0; i < RB; ++i)
+                wf[h][i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wsr, woff + i * 1024 + (k * 2 + h) * 4096, 0, 2));
 #pragma unroll
-            for (int i = 0; i < TB; ++i) xsc[u][i] = row_scales(p, from.s, source[i], k * 8 + (lane >> 4));
-        }
+        for (int h = 0; h < 2; ++h) wsc[h] = __builtin_amdgcn_raw_buffer_load_b32(ssr, soff + (k * 2 + h) * 256, 0, 0);
+#pragma unroll
+        for (int i = 0; i < TB; ++i) xsc[i] = row_scales(p, from.s, source[i], k * 8 + (lane >> 4));
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        auto half = [&](auto hh) {
+            constexpr int h = decltype(hh)::value;
+            i32x4 xf[TB];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            auto half = [&](auto hh) {
-                constexpr int h = decltype(hh)::value;
-                i32x4 xf[TB];
+            for (int j = 0; j < TB; ++j)
+                xf[j] = *reinterpret_cast<const i32x4*>(smem + at + j * 2048 + (((4 * h + (lane >> 4)) ^ (lane & 7)) << 4));
+            const unsigned ws = RB == 4 ? wsc[h] : wsc[h] >> (8 * (b0 & 3));
 #pragma unroll
-                for (int j = 0; j < TB; ++j)
-                    xf[j] = *reinterpret_cast<const i32x4*>(smem + at + u * TB * 2048 + j * 2048 + (((4 * h + (lane >> 4)) ^ (lane & 7)) << 4));
-                const unsigned ws = RB == 4 ? wsc[u][h] : wsc[u][h] >> (8 * (b0 & 3));
-#pragma unroll
-                for (int j = 0; j < TB; ++j) {
-                    acc[0][j] = mma4<0, h>(wf[u][h][0], xf[j], acc[0][j], ws, xsc[u][j]);
-                    if constexpr (RB >= 2) acc[1][j] = mma4<1, h>(wf[u][h][1], xf[j], acc[1][j], ws, xsc[u][j]);
-                    if constexpr (RB == 4) {
-                        acc[2][j] = mma4<2, h>(wf[u][h][2], xf[j], acc[2][j], ws, xsc[u][j]);
-                        acc[3][j] = mma4<3, h>(wf[u][h][3], xf[j], acc[3][j], ws, xsc[u][j]);
-                    }
+            for (int j = 0; j < TB; ++j) {
+                acc[0][j] = mma4<0, h>(wf[h][0], xf[j], acc[0][j], ws, xsc[j]);
+                if constexpr (RB >= 2) acc[1][j] = mma4<1, h>(wf[h][1], xf[j], acc[1][j], ws, xsc[j]);
+                if constexpr (RB == 4) {
+                    acc[2][j] = mma4<2, h>(wf[h][2], xf[j], acc[2][j], ws, xsc[j]);
+                    acc[3][j] = mma4<3, h>(wf[h][3], xf[j], acc[3][j], ws, xsc[j]);
                 }
-            };
-            half(std::integral_constant<int, 0>{});
-            half(std::integral_constant<int, 1>{});
-        }
+            }
+        };
+        half(std::integral_constant<int, 0>{});
+        half(std::integral_constant<int, 1>{});
         asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // read, before the next loads land there
     }
     __syncthreads();
@@ -532,10 +523,10 @@ inline int64_t tiles_of(const Mx4Product& p, int per)
     return p.rows / per + (p.experts < p.rows ? p.experts : p.rows);
 }
 
-template <int TB, int RB, int NW, int U>
+template <int TB, int RB, int NW>
 int launch_few4(const Mx4Product& p, hipStream_t s)
 {
-    constexpr int LDS = few4_lds<TB, RB, NW, U>();
+    constexpr int LDS = few4_lds<TB, RB, NW>();
     static_assert(LDS <= 64 * 1024, "more needs allow_lds");
     const int parts = p.groups * 4 / RB;
     const int64_t grid = tiles_of(p, 16 * TB) * parts;
@@ -543,22 +534,27 @@ int launch_few4(const Mx4Product& p, hipStream_t s)
         set_error("%lld workgroups: too many", (long long)grid);
         return NM_ERR_SHAPE;
     }
-    hipLaunchKernelGGL((mx4_few_kernel<TB, RB, NW, U>), dim3((unsigned)grid), dim3(NW * 64), LDS, s, p, parts);
+    hipLaunchKernelGGL((mx4_few_kernel<TB, RB, NW>), dim3((unsigned)grid), dim3(NW * 64), LDS, s, p, parts);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }
 
+// Bound by HBM: 16 rows of 12288 -> 4096 take 10.4 us, of which 3.5 are a call's that reads next to nothing and 5.9 the weights' at a copy's
+// rate.  A workgroup's blocks x wavefronts by how many row groups there are; us (16 rows; weights out of HBM):
+//   4096 -> 4096        64 groups   1 x 8  5.6     1 x 4   6.4     1 x 16   5.8     2 x 8   6.0
+//   12288 -> 4096       64          1 x 8 10.4     1 x 4  12.6     1 x 16  10.2     2 x 8  11.1     4 x 8  14.9
+//   28672 -> 8192      128          1 x 8 28.1     2 x 8  22.9     2 x 16  23.1     4 x 8  28.1
+//   4096 -> 2 x 12288  384          4 x 4 13.8     4 x 8  14.2     4 x 16  17.0
+//   64 experts, 1024 -> 2048, 128 entries   4 x 4 13.6   4 x 8  18.1   2 x 4  15.4   1 x 8  37
+// (Two or four steps in flight a wavefront: the same, but where k has too few for that: 64 experts as above 17.2.)
 template <int TB>
 int pick_few4(const Mx4Product& p, hipStream_t s)
 {
-    constexpr int U = TB == 4 ? 1 : 2;
     const int64_t groups = p.groups * (p.grouped ? (p.rows < p.experts ? p.rows : p.experts) : 1);
-    if (groups >= 192 || (p.out == NM_MX4 && p.gated)) return launch_few4<TB, 4, 4, U>(p, s);
-    if (groups >= 128 || p.out == NM_MX4) return launch_few4<TB, 2, 8, U>(p, s);
-    return launch_few4<TB, 1, 8, U>(p, s);
+    if (groups >= 192 || (p.out == NM_MX4 && p.gated)) return launch_few4<TB, 4, 4>(p, s);
+    if (groups >= 128 || p.out == NM_MX4) return launch_few4<TB, 2, 8>(p, s);
+    return launch_few4<TB, 1, 8>(p, s);
 }
-
-constexpr int kFewRows4 = 64;
 
 // What runs a call: a tile shape, or the few-row kernels (-1).
 struct Mx4Plan {
@@ -604,19 +600,27 @@ int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 
 }  // namespace
 
-// The shape with the least estimated time: rounds of workgroups over 256 CUs, two a CU.  Groups leave half a tile empty each.
+// Which kernel, by the rows (of a group, on average) and the groups that there are.
+// Up to 64 rows the tile kernels run where they have a workgroup for half of the CUs, and either 8 rows of an expert (whose numbers are uneven) or
+// more than 16 of one matrix.  us, few-row and tile kernel: 64 x 4096 -> 4096 10.6 and 12.9, -> 2 x 12288 22.4 and 22.9, -> 32768 27 and 24;
+// 4096 -> 65536 of 16 rows 26 and 30, 32 rows 34 and 31, 64 rows 50 and 35; 64 experts, 2048 -> 2 x 1024, of 2 rows each 17.5 and 20, 4 rows
+// 21.5 and 22, 16 rows 34 and 26, 32 rows 45 and 31; 60 experts, 1440 -> 1111, of 9 rows 15.4 and 12.6; 8 experts, 4096 -> 4096, of 16 rows 20 and 17.
+// Of the tile kernels that with the least estimated time: rounds of workgroups over 256 CUs, two a CU; each group leaves half a tile empty.
 // us, 128 rows and 64: 512 x 4096 -> 4096 17.4 and 13.3, 2048 x 4096 -> 8192 37 and 50, 8192 x 4096 -> 16384 270 and 330, 60 experts
 // of 12004 x 1440 -> 1111 37 and 35, 64 of 32768 x 2048 -> 2 x 1024 107 and 123.
 static Mx4Plan mx4_plan(const Mx4Product& p)
 {
     Mx4Plan pl;
-    const int64_t each = p.grouped ? (p.rows + p.experts - 1) / p.experts : p.rows;
-    if (each <= kFewRows4 || p.blocks < 4) return pl;   // (the tile kernels read scales by fours)
+    const int groups = !p.grouped ? 1 : p.experts < p.rows ? p.experts : p.rows;
+    const int each = (p.rows + groups - 1) / groups;
+    const bool wide = (int64_t)groups * ((p.groups + 3) / 4) >= 128;
+    if (p.blocks < 4) return pl;   // (the tile kernels read scales by fours)
+    if (each <= 64 && !(wide && each >= (p.grouped ? 8 : 17))) return pl;
     float least = 1e30f;
     for (int sh = 0; sh < (int)(sizeof(kShapes4) / sizeof(Shape4)); ++sh) {
         const Shape4& k = kShapes4[sh];
-        const int64_t groups = p.grouped ? p.experts : 0;
-        const int64_t tiles = (groups ? p.rows / k.rows + (groups + 1) / 2 : (p.rows + k.rows - 1) / k.rows) * ((p.groups + k.wr - 1) / k.wr);
+        const int64_t tall = !p.grouped ? (p.rows + k.rows - 1) / k.rows : p.rows / k.rows + (groups + 1) / 2;
+        const int64_t tiles = (tall < groups ? groups : tall) * ((p.groups + k.wr - 1) / k.wr);
         const int64_t rounds = tiles / 512, rest = tiles % 512;
         const float us = rounds * (k.fixed + p.steps * k.shared) + (rest ? k.fixed + p.steps * (rest > 256 ? k.shared : k.alone) : 0.0f);
         if (us < least) {
