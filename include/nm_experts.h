@@ -13,7 +13,7 @@
 extern "C" {
 #endif
 
-enum { NM_ROUTE_MAX_EXPERTS = 1024, NM_ROUTE_MAX_CHOICES = 64 };
+enum { NM_ROUTE_MAX_EXPERTS = 1024, NM_ROUTE_MAX_CHOICES = 64, NM_ROUTE_ONE_LAUNCH = 64 };
 
 /*
  * nm_route -- each token's `choices` largest logits and the order of the tokens by expert:
@@ -29,7 +29,7 @@ enum { NM_ROUTE_MAX_EXPERTS = 1024, NM_ROUTE_MAX_CHOICES = 64 };
  *   logits_dev   rows of dtype (NM_F32 or NM_BF16) at stride ld
  *   1 <= experts <= NM_ROUTE_MAX_EXPERTS, 1 <= choices <= min(experts, NM_ROUTE_MAX_CHOICES), 0 <= tokens * choices < 2^31
  *   (no tokens: offsets are still written)
- *   workspace_dev  at least nm_route_workspace() bytes, 16-byte aligned
+ *   workspace_dev  at least nm_route_workspace() bytes, 16-byte aligned (none for up to NM_ROUTE_ONE_LAUNCH tokens)
  */
 int nm_route(const void* logits_dev, nm_dtype_t dtype, int64_t tokens, int experts, int64_t ld, int choices, int normalise,
              int32_t* ids_dev, float* weights_dev, int32_t* offsets_dev, int32_t* rows_dev, int32_t* slots_dev,

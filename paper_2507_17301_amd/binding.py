@@ -17,7 +17,7 @@ import numpy as np
 NM_F32, NM_BF16, NM_F8E4M3, NM_I8, NM_MX4 = 0, 1, 2, 3, 4
 NM_Q8_MAX_WIDTH, NM_Q8_FEW_ROWS = 65536, 64
 NM_MX4_MAX_WIDTH, NM_MX4_MAX_EXPERTS = 65536, 1024
-NM_ROUTE_MAX_EXPERTS, NM_ROUTE_MAX_CHOICES = 1024, 64
+NM_ROUTE_MAX_EXPERTS, NM_ROUTE_MAX_CHOICES, NM_ROUTE_ONE_LAUNCH = 1024, 64, 64
 NM_OK = 0
 NM_ERR_ARG, NM_ERR_SHAPE, NM_ERR_UNSUPPORTED, NM_ERR_ALLOC, NM_ERR_HIP, NM_ERR_IO = -1, -2, -3, -4, -5, -6
 _STATUS = {0: "NM_OK", -1: "NM_ERR_ARG", -2: "NM_ERR_SHAPE", -3: "NM_ERR_UNSUPPORTED",
@@ -699,7 +699,8 @@ def _mx4_rows_of(q, scales, dev: int):
         raise TypeError(f"q must be uint8, not {q.dtype}")
     if nbytes % 16:
         raise ValueError(f"rows of q have whole blocks of 16 bytes, not {nbytes} bytes")
-    return rows, nbytes // 16, ldq, _q8_stride(scales, "scales", q.shape[:-1] + (nbytes // 16,), _torch.uint8, dev)
+    nb = nbytes >> 4
+    return rows, nb, ldq, _q8_stride(scales, "scales", (rows, nb) if q.dim() == 2 else q.shape[:-1] + (nb,), _torch.uint8, dev)
 
 
 def _mx4_out(x, lead, width: int, q, scales, dev: int, names=("q", "scales")):
@@ -931,16 +932,19 @@ def nm_route(logits, k: int, normalise: bool = True, stream=None) -> Routing:
             return nm_route(logits, k, normalise)
     L = _lib or lib()
     tokens, experts, ld = _rows_of(logits, "logits")
-    dev, lead = logits.get_device(), logits.shape[:-1]
-    i32 = _torch.int32
-    ids, weights, slots = (logits.new_empty(lead + (k,), dtype=t) for t in (i32, _torch.float32, i32))
-    offsets, rows = logits.new_empty((experts + 1,), dtype=i32), logits.new_empty((tokens * k,), dtype=i32)
-    need = ctypes.c_size_t(0)
-    _check(L.nm_route_workspace(tokens, experts, ctypes.byref(need)))
-    ws = logits.new_empty(need.value, dtype=_torch.uint8) if need.value else None
+    dev, i32 = logits.get_device(), _torch.int32
+    ids, weights, slots = logits.new_empty((3,) + logits.shape[:-1] + (k,), dtype=i32).unbind()   # (one allocation instead of three)
+    weights = weights.view(_torch.float32)
+    offsets, rows = logits.new_empty(experts + 1 + tokens * k, dtype=i32).split_with_sizes((experts + 1, tokens * k))
+    nbytes, ws = 0, None
+    if tokens > NM_ROUTE_ONE_LAUNCH:   # (else none is needed)
+        need = ctypes.c_size_t(0)
+        _check(L.nm_route_workspace(tokens, experts, ctypes.byref(need)))
+        nbytes = need.value
+        ws = logits.new_empty(nbytes, dtype=_torch.uint8)
     rc = L.nm_route_args(_ROUTE_ARGS.pack(logits.data_ptr(), ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(),
                                           0 if ws is None else ws.data_ptr(), _q8_stream(dev), _q8_code(logits.dtype, "logits"), tokens, experts, ld, k,
-                                          bool(normalise), need.value))
+                                          bool(normalise), nbytes))
     if rc < 0:
         _check(rc)
     return Routing(ids, weights, offsets, rows, slots)

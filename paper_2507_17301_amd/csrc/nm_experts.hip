@@ -10,7 +10,8 @@ namespace {
 // doubles finds the largest logit and of equal ones the lowest expert.  The choices are taken one after another.
 // The order by expert comes of one 64-bit mask an expert and batch, with a bit for each token that chose it: an expert's count is the number of
 // its bits, a token's place among the batch's the number of bits below its own.  So no order of atomics shows in a result.
-constexpr int kThreads = 1024, kBatch = 64, kChunks = 256;
+constexpr int kThreads = 1024, kBatch = NM_ROUTE_ONE_LAUNCH, kChunks = 256;
+static_assert(kBatch == 64, "a bit for each token");
 
 template <int CTRL> __device__ inline unsigned dpp(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
 
