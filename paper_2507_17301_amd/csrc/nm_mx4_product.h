@@ -26,49 +26,66 @@ struct RowTile {
 struct GroupTiles {
     int per, each, mine, upto;   // groups of a lane; tiles of its groups, and of those and all before
     int all;
+    int first, count;            // row and rows of the lane's first group
 
     // (values outside the rows of y count as the nearer end)
-    static __device__ inline int begin(const Mx4Product& p, int e) { return e < p.experts ? min(max(p.offsets[e], 0), p.rows) : 0; }
-    static __device__ inline int rows(const Mx4Product& p, int e) { return e < p.experts ? max(min(max(p.offsets[e + 1], 0), p.rows) - begin(p, e), 0) : 0; }
+    static __device__ inline void range(const Mx4Product& p, int e, int& begin, int& n)
+    {
+        const int in = e < p.experts ? e : p.experts - 1;
+        begin = min(max(p.offsets[in], 0), p.rows);
+        const int end = min(max(p.offsets[in + 1], 0), p.rows);
+        n = e < p.experts ? max(end - begin, 0) : 0;
+    }
+    // the sum of a lane's v and of all lanes' before it
+    static __device__ inline int scan(int v)
+    {
+        v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // within sixteen lanes: the one 1 below,
+        v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);   // 2,
+        v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);   // 4
+        v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);   // and 8 below
+        v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // the last of lanes 0 - 15 and 32 - 47 to the sixteen after
+        v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
+        return v;
+    }
     __device__ inline GroupTiles(const Mx4Product& p, int tile_rows) : per(tile_rows), each((p.experts + 63) >> 6)
     {
         const int lane = threadIdx.x & 63;
-        int m = 0, to = 0, n = (int)((p.rows + (int64_t)tile_rows - 1) / tile_rows);
+        int m = 0, to = 0, n = (int)((p.rows + (int64_t)tile_rows - 1) / tile_rows), b0 = 0, n0 = 0;
         if (p.grouped) {
+            range(p, lane * each, b0, n0);
+            m = (n0 + tile_rows - 1) / tile_rows;
 #pragma unroll 4
-            for (int i = 0; i < each; ++i) m += (rows(p, lane * each + i) + tile_rows - 1) / tile_rows;
-            to = m;
-            for (int d = 1; d < 64; d <<= 1) {
-                const int up = __shfl_up(to, d);
-                to += lane >= d ? up : 0;
+            for (int i = 1; i < each; ++i) {
+                int b, k;
+                range(p, lane * each + i, b, k);
+                m += (k + tile_rows - 1) / tile_rows;
             }
+            to = scan(m);
             n = __builtin_amdgcn_readlane(to, 63);
         }
         mine = m;
         upto = to;
         all = n;
+        first = b0;
+        count = n0;
     }
     // Tile number `tile`; count is 0 past the last one.
     __device__ inline RowTile at(const Mx4Product& p, int tile) const
     {
-        int expert = 0, row0 = tile * per, count = max(min(p.rows - row0, per), 0);
-        if (p.grouped) {
-            int before = upto - mine;
-            count = 0;
-            for (int i = 0; i < each; ++i) {   // (every lane as if the tile were of its groups)
-                const int e = (threadIdx.x & 63) * each + i, n = rows(p, e), in = tile - before;
-                const bool here = in >= 0 && in * (int64_t)per < n;
-                expert = here ? e : expert;
-                row0 = here ? begin(p, e) + in * per : row0;
-                count = here ? min(n - in * per, per) : count;
-                before += (n + per - 1) / per;
-            }
-            const int l = tile < all ? __ffsll(__ballot(upto > tile)) - 1 : 0;
-            expert = __builtin_amdgcn_readlane(expert, l);
-            row0 = __builtin_amdgcn_readlane(row0, l);
-            count = tile < all ? __builtin_amdgcn_readlane(count, l) : 0;
+        if (!p.grouped) return {0, __builtin_amdgcn_readfirstlane(max(min(p.rows - tile * per, per), 0)), __builtin_amdgcn_readfirstlane(tile * per)};
+        int expert = 0, row0 = 0, n = 0, before = upto - mine;
+        for (int i = 0; i < each; ++i) {   // (every lane as if the tile were of its groups)
+            const int e = (threadIdx.x & 63) * each + i, in = tile - before;
+            int b = first, k = count;
+            if (i) range(p, e, b, k);
+            const bool here = in >= 0 && in * (int64_t)per < k;
+            expert = here ? e : expert;
+            row0 = here ? b + in * per : row0;
+            n = here ? min(k - in * per, per) : n;
+            before += (k + per - 1) / per;
         }
-        return {__builtin_amdgcn_readfirstlane(expert), __builtin_amdgcn_readfirstlane(count), __builtin_amdgcn_readfirstlane(row0)};
+        const int l = tile < all ? __ffsll(__ballot(upto > tile)) - 1 : 0;
+        return {__builtin_amdgcn_readlane(expert, l), tile < all ? __builtin_amdgcn_readlane(n, l) : 0, __builtin_amdgcn_readlane(row0, l)};
     }
 };
 
