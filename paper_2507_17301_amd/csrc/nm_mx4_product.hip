@@ -569,7 +569,7 @@ struct Shape4 {
     float fixed, alone, shared;       // us: of a tile; of a step with one workgroup a CU, with two
 };
 constexpr Shape4 kShapes4[] = {{4, 128, 4, 2, 5.5f, 0.70f, 1.80f},    // 256 packed channels x 128 rows
-                               {4, 64, 4, 2, 5.0f, 0.49f, 1.25f}};
+                               {4, 64, 4, 2, 5.0f, 0.49f, 1.15f}};
 
 template <int SHAPE, int TB, int NS, bool GATED, int OUT>
 int launch_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
@@ -605,9 +605,11 @@ int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 // more than 16 of one matrix.  us, few-row and tile kernel: 64 x 4096 -> 4096 10.6 and 12.9, -> 2 x 12288 22.4 and 22.9, -> 32768 27 and 24;
 // 4096 -> 65536 of 16 rows 26 and 30, 32 rows 34 and 31, 64 rows 50 and 35; 64 experts, 2048 -> 2 x 1024, of 2 rows each 17.5 and 20, 4 rows
 // 21.5 and 22, 16 rows 34 and 26, 32 rows 45 and 31; 60 experts, 1440 -> 1111, of 9 rows 15.4 and 12.6; 8 experts, 4096 -> 4096, of 16 rows 20 and 17.
-// Of the tile kernels that with the least estimated time: rounds of workgroups over 256 CUs, two a CU; each group leaves half a tile empty.
+// Of the tile kernels that with the least estimated time: rounds of workgroups over 256 CUs, two a CU; a group leaves five eighths of a tile empty (half,
+// but for those of fewer rows than a tile).
 // us, 128 rows and 64: 512 x 4096 -> 4096 17.4 and 13.3, 2048 x 4096 -> 8192 37 and 50, 8192 x 4096 -> 16384 270 and 330, 60 experts
-// of 12004 x 1440 -> 1111 37 and 35, 64 of 32768 x 2048 -> 2 x 1024 107 and 123.
+// of 12004 x 1440 -> 1111 35 and 35, 64 of 4096 x 2048 -> 2 x 1024 36 and 32, of 32768 103 and 120.
+// (One workgroup after another on a CU's slots, the next tile asked for before the last is stored: 0 to 16 % slower.)
 static Mx4Plan mx4_plan(const Mx4Product& p)
 {
     Mx4Plan pl;
@@ -619,7 +621,7 @@ static Mx4Plan mx4_plan(const Mx4Product& p)
     float least = 1e30f;
     for (int sh = 0; sh < (int)(sizeof(kShapes4) / sizeof(Shape4)); ++sh) {
         const Shape4& k = kShapes4[sh];
-        const int64_t tall = !p.grouped ? (p.rows + k.rows - 1) / k.rows : p.rows / k.rows + (groups + 1) / 2;
+        const int64_t tall = !p.grouped ? (p.rows + k.rows - 1) / k.rows : p.rows / k.rows + (groups * (int64_t)5 + 7) / 8;
         const int64_t tiles = (tall < groups ? groups : tall) * ((p.groups + k.wr - 1) / k.wr);
         const int64_t rounds = tiles / 512, rest = tiles % 512;
         const float us = rounds * (k.fixed + p.steps * k.shared) + (rest ? k.fixed + p.steps * (rest > 256 ? k.shared : k.alone) : 0.0f);
