@@ -107,7 +107,8 @@ int nm_linear_mx4(const uint8_t* q_dev, int64_t ldq, const uint8_t* scales_dev, 
  * nm_linear_mx4 with expert e's weights and bias, of row r of x, or of row index[r] where an index is given.
  *   offsets_dev     int32 [experts + 1] on the device, not falling, from 0 to at most `entries` (as nm_route writes them).
  *                   Groups may be empty.  Values outside [0, entries] count as the nearer end, a group that ends before
- *                   it begins as empty.  Rows of y in no group are left as they were.
+ *                   it begins as empty.  Rows of y in no group are left as they were; where offsets fall, a row in
+ *                   several groups holds what one of them gives or is left, too.
  *   index_dev       int32 [entries], or NULL.  An index outside [0, rows) makes its row of y NaN.
  *   entries         rows of y (without an index: also of x, rows = entries)
  *   bias_dev        fp32 [experts][channels], or NULL

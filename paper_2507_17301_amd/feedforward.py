@@ -82,6 +82,8 @@ class ExpertsMX4:
     def forward(self, x, logits, residual=None, stream=None):
         """x, residual: [..., width] in bf16 or fp32 (x: the normalised rows); logits [..., experts].  Returns residual plus the
         experts' answers, shaped and typed like x.  The answers that are summed are bf16 for bf16 rows, fp32 for fp32."""
+        if x.shape[:-1] != logits.shape[:-1] or logits.shape[-1] != self.up.experts:
+            raise ValueError(f"rows {tuple(x.shape)} and logits {tuple(logits.shape)} for {self.up.experts} experts do not fit together")
         to = nm.nm_route(logits, self.k, self.normalise, stream=stream)
         q, s = nm.nm_quantize_mx4(x, stream=stream)
         q, s = nm.nm_experts_mx4(q, s, self.up, to.offsets, to.rows, rounded=True, stream=stream)

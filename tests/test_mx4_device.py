@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2507_17301_amd import binding as nm
+from paper_2507_17301_amd.feedforward import ExpertsMX4, FeedForwardMX4
 from test_q8_device import Tensor, machine, pytestmark  # noqa: F401  (the fixture and the mark)
 
 
@@ -58,3 +59,25 @@ def test_one_tensor_of_another_device_is_refused(machine, name):  # noqa: F811
         nm.nm_experts_mx4(Tensor((3, 32), u8, 0), Tensor((3, 2), u8, at("scales")), nm.MX4Weights(None, 2, 64, 64, False), Tensor((3,), i32, at("offsets")),
                           Tensor((3,), i32, at("rows")), Tensor((2, 64), torch.float32, at("bias")), y=Tensor((3, 64), torch.float32, at("y")))
     assert machine.launches == 0
+
+
+def _weights(experts, channels, width, gated):
+    return nm.MX4Weights(None, experts, channels, width, gated)
+
+
+@pytest.mark.parametrize("x,logits", [((5, 64), (4, 3)), ((4, 64), (5, 3)), ((2, 2, 64), (4, 3)), ((4, 64), (4, 2)), ((4, 64), (4, 4))])
+def test_rows_and_logits_that_do_not_fit_together_are_refused(machine, x, logits):  # noqa: F811
+    layer = ExpertsMX4(_weights(3, 128, 64, True), _weights(3, 64, 64, False), 2)
+    with pytest.raises(ValueError, match="do not fit together"):
+        layer(Tensor(x, torch.float32, 0), Tensor(logits, torch.float32, 0))
+    assert machine.launches == 0
+
+
+def test_weights_that_do_not_fit_together_are_refused():
+    up, down = _weights(3, 128, 64, True), _weights(3, 64, 64, False)
+    for a, b, k in ((down, down, 2), (up, up, 2), (up, _weights(3, 64, 96, False), 2), (up, _weights(3, 96, 64, False), 2), (up, _weights(2, 64, 64, False), 2), (up, down, 0),
+                    (up, down, 4)):
+        with pytest.raises(ValueError):
+            ExpertsMX4(a, b, k)
+    with pytest.raises(ValueError):
+        FeedForwardMX4(None, up, down)
