@@ -110,15 +110,14 @@ struct RowBuffers {
     }
 };
 
-// The two scales of a row that a lane needs in a step, as the low bytes of a word: blocks kb and kb + 4.  Past the row's blocks 1 (the
-// codes there meet zeros), for an index outside x NaN.
-__device__ inline unsigned row_scales(const Mx4Product& p, __amdgpu_buffer_rsrc_t s, int source, int kb)
+// The scales of a row's last step, of which `have` < 8 are there; the others are 1 (the codes there meet zeros).
+__device__ inline u32x2 last_scales(const uint8_t* from, int have)
 {
-    if (source == -2) return 0xffffu;
-    const unsigned at = source < 0 ? kPast : (unsigned)(source * p.lds) + kb;
-    const unsigned a = __builtin_amdgcn_raw_buffer_load_b8(s, kb < p.blocks ? at : kPast, 0, 0);
-    const unsigned b = __builtin_amdgcn_raw_buffer_load_b8(s, kb + 4 < p.blocks ? at + 4 : kPast, 0, 0);
-    return (kb < p.blocks ? a : 127u) | (kb + 4 < p.blocks ? b : 127u) << 8;
+    u32x2 v = {0x7f7f7f7fu, 0x7f7f7f7fu};
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < have) v[i >> 2] = (v[i >> 2] & ~(0xffu << (8 * (i & 3)))) | (unsigned)from[i] << (8 * (i & 3));
+    return v;
 }
 
 // What a lane needs of the channels it holds over NB blocks (from block b0 on) of one row group: one run of adjacent outputs, or two.

@@ -39,7 +39,10 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
     const unsigned mine = wave * (TB * 2048), lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem + mine;
     const unsigned at = mine + (lane & 15) * 128;
     unsigned qoff[TB][2];   // 8 rows an instruction, block c of a row at c ^ (row & 7)
-    int source[TB];
+    // A step's eight scales of a row: one load of a lane for each of the tile's rows, dealt out among the lanes.
+    const int source = source_of(p, t, lane & (16 * TB - 1));
+    const uint8_t* scales = p.s + (p.index ? 0 : (int64_t)t.row0 * p.lds) + (source < 0 ? 0 : source) * p.lds;
+    const unsigned pick = 0x0c0c0400u + (lane >> 4) * 0x0101u;   // of two words the byte of the lane's block each
     const int chunk = (lane & 7) ^ (lane >> 3);
 #pragma unroll
     for (int i = 0; i < TB; ++i) {
@@ -48,7 +51,6 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
             const int src = source_of(p, t, i * 16 + h * 8 + (lane >> 3));
             qoff[i][h] = src < 0 ? kPast : (unsigned)(src * p.ldq) + chunk * 16;
         }
-        source[i] = source_of(p, t, i * 16 + (lane & 15));
     }
     f32x4 acc[RB][TB] = {};
     for (int k = wave; k < p.steps; k += NW) {
@@ -67,9 +69,16 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
                 wf[h][i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wsr, woff + i * 1024 + (k * 2 + h) * 4096, 0, 2));
 #pragma unroll
         for (int h = 0; h < 2; ++h) wsc[h] = __builtin_amdgcn_raw_buffer_load_b32(ssr, soff + (k * 2 + h) * 256, 0, 0);
-#pragma unroll
-        for (int i = 0; i < TB; ++i) xsc[i] = row_scales(p, from.s, source[i], k * 8 + (lane >> 4));
+        u32x2 s8;
+        if (k * 8 + 8 <= p.blocks) __builtin_memcpy(&s8, scales + k * 8, 8);
+        else s8 = last_scales(scales + k * 8, p.blocks - k * 8);
+        if (source == -2) s8 = u32x2{0xffffffffu, 0xffffffffu};
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+#pragma unroll
+        for (int i = 0; i < TB; ++i) {
+            const unsigned lo = TB == 1 ? s8[0] : __shfl(s8[0], i * 16 + (lane & 15)), hi = TB == 1 ? s8[1] : __shfl(s8[1], i * 16 + (lane & 15));
+            xsc[i] = __builtin_amdgcn_perm(hi, lo, pick);
+        }
         auto half = [&](auto hh) {
             constexpr int h = decltype(hh)::value;
             i32x4 xf[TB];
@@ -529,7 +538,11 @@ template <int TB, int RB, int NW>
 int launch_few4(const Mx4Product& p, hipStream_t s)
 {
     constexpr int LDS = few4_lds<TB, RB, NW>();
-    static_assert(LDS <= 64 * 1024, "more needs allow_lds");
+    if constexpr (LDS > 64 * 1024) {
+        static unsigned long long done = 0;
+        const int rc = allow_lds((const void*)mx4_few_kernel<TB, RB, NW>, LDS, &done);
+        if (rc != NM_OK) return rc;
+    }
     const int parts = p.groups * 4 / RB;
     const int64_t grid = tiles_of(p, 16 * TB) * parts;
     if (grid > 0x7fffffff) {
@@ -541,20 +554,35 @@ int launch_few4(const Mx4Product& p, hipStream_t s)
     return NM_OK;
 }
 
-// Bound by HBM: 16 rows of 12288 -> 4096 take 10.4 us, of which 3.5 are a call's that reads next to nothing and 5.9 the weights' at a copy's
-// rate.  A workgroup's blocks x wavefronts by how many row groups there are; us (16 rows; weights out of HBM):
-//   4096 -> 4096        64 groups   1 x 8  5.6     1 x 4   6.4     1 x 16   5.8     2 x 8   6.0
-//   12288 -> 4096       64          1 x 8 10.4     1 x 4  12.6     1 x 16  10.2     2 x 8  11.1     4 x 8  14.9
-//   28672 -> 8192      128          1 x 8 28.1     2 x 8  22.9     2 x 16  23.1     4 x 8  28.1
-//   4096 -> 2 x 12288  384          4 x 4 13.8     4 x 8  14.2     4 x 16  17.0
-//   64 experts, 1024 -> 2048, 128 entries   4 x 4 13.6   4 x 8  18.1   2 x 4  15.4   1 x 8  37
-// (Two or four steps in flight a wavefront: the same, but where k has too few for that: 64 experts as above 17.2.)
+// Groups of 64 packed channels times tiles of `per` rows, were the rows dealt evenly.
+inline int64_t places(const Mx4Product& p, int per)
+{
+    const int groups = !p.grouped ? 1 : p.experts < p.rows ? p.experts : p.rows;
+    const int each = (p.rows + groups - 1) / groups;
+    return (int64_t)groups * ((each + per - 1) / per) * p.groups;
+}
+
+// Up to 16 rows bound by HBM: 12288 -> 4096 takes 9.0 us, of which 3.5 are a call's that reads next to nothing and 5.9 the weights' at a copy's rate.  Of
+// more rows by the vector memory unit of a CU, through which a workgroup's rows of x go as its weights do (64 rows of 12288 -> 4096: 16.0; with
+// each scale of a row loaded by itself 22.3).  So as many channels a workgroup as leave one for most CUs.  us, row blocks x wavefronts:
+//   rows     weights          places    1 x 8   2 x 8   4 x 8   4 x 4
+//     16    4096 ->  4096        64       5.6     6.0
+//     16   12288 ->  4096        64       8.9    11.1    14.5    14.6
+//     64   12288 ->  4096        64      16.1    18.5    23.8    25.1
+//     64    8192 ->  8192       128      19.9    14.9    18.1    18.8
+//    128   12288 ->  4096       128      27.1    17.9    22.7    23.9
+//     16    4096 -> 12288       192              10.7     8.4     9.1
+//    200   12288 ->  4096       256      44.9    31.3    22.5    23.1
+//     64    4096 -> 32768       512              27.3    25.1    22.2
+//   64 experts, 1024 -> 2048, 256 entries                17.7    14.8
+// (Two or four steps in flight a wavefront: the same, but where k has too few for that.  Wavefronts of different workgroups at different steps at a time:
+// the same.)
 template <int TB>
 int pick_few4(const Mx4Product& p, hipStream_t s)
 {
-    const int64_t groups = p.groups * (p.grouped ? (p.rows < p.experts ? p.rows : p.experts) : 1);
-    if (groups >= 192 || (p.out == NM_MX4 && p.gated)) return launch_few4<TB, 4, 4>(p, s);
-    if (groups >= 128 || p.out == NM_MX4) return launch_few4<TB, 2, 8>(p, s);
+    const int64_t n = places(p, 16 * TB);
+    if (n >= 192 || (p.out == NM_MX4 && p.gated)) return n <= 256 ? launch_few4<TB, 4, 8>(p, s) : launch_few4<TB, 4, 4>(p, s);
+    if (n >= 128 || p.out == NM_MX4) return launch_few4<TB, 2, 8>(p, s);
     return launch_few4<TB, 1, 8>(p, s);
 }
 
@@ -602,11 +630,12 @@ int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 
 }  // namespace
 
-// Which kernel, by the rows (of a group, on average) and the groups that there are.
-// Up to 64 rows the tile kernels run where they have a workgroup for half of the CUs, and either 8 rows of an expert (whose numbers are uneven) or
-// more than 16 of one matrix.  us, few-row and tile kernel: 64 x 4096 -> 4096 10.6 and 12.9, -> 2 x 12288 22.4 and 22.9, -> 32768 27 and 24;
-// 4096 -> 65536 of 16 rows 26 and 30, 32 rows 34 and 31, 64 rows 50 and 35; 64 experts, 2048 -> 2 x 1024, of 2 rows each 17.5 and 20, 4 rows
-// 21.5 and 22, 16 rows 34 and 26, 32 rows 45 and 31; 60 experts, 1440 -> 1111, of 9 rows 15.4 and 12.6; 8 experts, 4096 -> 4096, of 16 rows 20 and 17.
+// Which kernel, by the rows (of a group, on average) and by the places that there are for workgroups.
+// The few-row kernels up to one workgroup a CU (whatever the rows: the tile kernels' few workgroups would take all of K one after another), of one matrix
+// also up to 32 rows and, of 640 places at most, 64; of experts up to 10 rows (whose numbers are uneven).  us, few-row and tile kernel:
+//   128 x 12288 -> 4096 17.9 and 46, 200 x 4096 -> 4096 11.0 and 12.9, 333 x 4096 -> 4096 17 and 13, 128 x 8192 -> 8192 17.9 and 32, 128 x 4096
+//   -> 10240 18.5 and 18.8, 32 x 4096 -> 65536 30 and 31, 48 rows 37 and 32, 64 x 4096 -> 32768 22 and 25; 64 experts, 2048 -> 2 x 1024, of 8 rows each
+//   28 and 32, 16 rows 34 and 32, 1024 -> 2048 15.8 and 15.7, 22 and 15.9; 60 experts, 1440 -> 1111, of 9 rows 13.9 and 15.4.
 // Of the tile kernels that with the least estimated time: rounds of workgroups over 256 CUs, two a CU; a group leaves five eighths of a tile empty (half,
 // but for those of fewer rows than a tile).
 // us, 128 rows and 64: 512 x 4096 -> 4096 17.4 and 13.3, 2048 x 4096 -> 8192 37 and 50, 8192 x 4096 -> 16384 270 and 330, 60 experts
@@ -617,9 +646,9 @@ static Mx4Plan mx4_plan(const Mx4Product& p)
     Mx4Plan pl;
     const int groups = !p.grouped ? 1 : p.experts < p.rows ? p.experts : p.rows;
     const int each = (p.rows + groups - 1) / groups;
-    const bool wide = (int64_t)groups * ((p.groups + 3) / 4) >= 128;
+    const int64_t n = places(p, 64);
     if (p.blocks < 4) return pl;   // (the tile kernels read scales by fours)
-    if (each <= 64 && !(wide && each >= (p.grouped ? 8 : 17))) return pl;
+    if (n <= 256 || each <= (p.grouped ? 10 : 32) || (!p.grouped && each <= 64 && n <= 640)) return pl;
     float least = 1e30f;
     for (int sh = 0; sh < (int)(sizeof(kShapes4) / sizeof(Shape4)); ++sh) {
         const Shape4& k = kShapes4[sh];

@@ -39,11 +39,43 @@ def test_long_rows(rows, k, n, gated):
     assert torch.isnan(z[rows // 2]).all() and torch.equal(z[rest], y[rest])
 
 
+# the smallest sizes whose tiles fill more than the chip once, and some that fill it several times; widths at the ends of blocks, words of scales, steps
+@pytest.mark.parametrize("rows,n", [(1025, 1100), (1153, 1030), (4100, 2600)])
+@pytest.mark.parametrize("k", [97, 128, 255, 256, 257, 512, 513, 1037])
 @pytest.mark.parametrize("gated", [False, True])
-@pytest.mark.parametrize("rows", [1, 16, 17, 40, 64, 65])
+def test_tiles(rows, n, k, gated):
+    g = torch.Generator().manual_seed(rows + k)
+    q, s = random_mx4(g, (rows, k))
+    w, ws = random_mx4(g, (n, k), 110, 122)
+    bias = torch.randn(n, generator=g) if k % 2 else None
+    say(f"linear_mx4 {rows} x {k} x {n} gated {gated}")
+    h = nm.nm_mx4_pack(w.cuda(), ws.cuda(), k, gated=gated)
+    b = None if bias is None else bias.cuda()
+    ref = product_ref(values_of(q, s, k), values_of(w, ws, k), bias, gated=gated)
+    y = nm.nm_linear_mx4(q.cuda(), s.cuda(), h, b, dtype=torch.float32)
+    check(y, ref)
+    check(nm.nm_linear_mx4(q.cuda(), s.cuda(), h, b), ref)
+    check(nm.nm_linear_mx4(q.cuda(), s.cuda(), h, b, rounded=True), ref)
+    if not gated:
+        r = torch.randn((rows, n), generator=g).bfloat16()
+        check(nm.nm_linear_mx4(q.cuda(), s.cuda(), h, b, r.cuda()), product_ref(values_of(q, s, k), values_of(w, ws, k), bias, r))
+    # a row that is not a number touches no other; nor do codes past the width
+    bad = s.clone()
+    bad[3, 0] = bad[rows - 1, -1] = 255
+    z = nm.nm_linear_mx4(q.cuda(), bad.cuda(), h, b, dtype=torch.float32)
+    rest = torch.ones(rows, dtype=torch.bool)
+    rest[3] = rest[rows - 1] = False
+    assert torch.isnan(z[~rest]).all() and torch.equal(z[rest], y[rest])
+    if k % 32:
+        q[:, (k + 1) // 2:] = 0x77
+        assert torch.equal(nm.nm_linear_mx4(q.cuda(), s.cuda(), h, b, dtype=torch.float32), y)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows", [1, 16, 17, 32, 33, 64, 65])
 def test_few_rows_of_wide_matrices(rows, gated):
     g = torch.Generator().manual_seed(rows)
-    k, n = 128, 32770
+    k, n = 128, 41000        # (more than 640 groups of 64 channels)
     q, s = random_mx4(g, (rows, k))
     w, ws = random_mx4(g, (n, k), 110, 122)
     say(f"linear_mx4 {rows} x {k} x {n} gated {gated}")
