@@ -98,17 +98,12 @@ __device__ inline int source_of(const Mx4Product& p, const RowTile& t, int row)
     return (unsigned)at < (unsigned)p.sources ? at : -2;   // -2: an index outside x
 }
 
-// The buffers of codes and scales of a tile's rows.
-struct RowBuffers {
-    __amdgpu_buffer_rsrc_t q, s;
-    __device__ inline RowBuffers(const Mx4Product& p, const RowTile& t)
-    {
-        const int64_t first = p.index ? 0 : t.row0;
-        const int64_t rows = p.index ? p.sources : t.count;
-        q = q8_rsrc(p.q + first * p.ldq, (unsigned)((rows - 1) * p.ldq + p.blocks * 16));
-        s = q8_rsrc(p.s + first * p.lds, (unsigned)((rows - 1) * p.lds + p.blocks));
-    }
-};
+// The buffer of the codes of a tile's rows.
+__device__ inline __amdgpu_buffer_rsrc_t row_buffer(const Mx4Product& p, const RowTile& t)
+{
+    const int64_t first = p.index ? 0 : t.row0, rows = p.index ? p.sources : t.count;
+    return q8_rsrc(p.q + first * p.ldq, (unsigned)((rows - 1) * p.ldq + p.blocks * 16));
+}
 
 // The scales of a row's last step, of which `have` < 8 are there; the others are 1 (the codes there meet zeros).
 __device__ inline u32x2 last_scales(const uint8_t* from, int have)

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
     const size_t group = (size_t)t.expert * p.groups + (b0 >> 2);
     const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + group * p.steps * 8192, (unsigned)p.steps * 8192);
     const __amdgpu_buffer_rsrc_t ssr = q8_rsrc(p.ws + group * p.steps * 128, (unsigned)p.steps * 512);
-    const RowBuffers from(p, t);
+    const __amdgpu_buffer_rsrc_t qsr = row_buffer(p, t);
     const unsigned woff = (b0 & 3) * 1024 + lane * 16, soff = lane * 4;
     const unsigned mine = wave * (TB * 2048), lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem + mine;
     const unsigned at = mine + (lane & 15) * 128;
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
         for (int i = 0; i < TB; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                load_to_lds(from.q, row_in && qoff[i][h] != kPast ? qoff[i][h] + k * 128 : kPast, lds0 + i * 2048 + h * 1024);
+                load_to_lds(qsr, row_in && qoff[i][h] != kPast ? qoff[i][h] + k * 128 : kPast, lds0 + i * 2048 + h * 1024);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4P
     const size_t group = (size_t)t.expert * p.groups + (own ? g0 + wave : 0);
     const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + group * halves * 4096, own ? (unsigned)halves * 4096 : 0);
     const __amdgpu_buffer_rsrc_t gsr = q8_rsrc(p.ws + group * halves * 64, own ? (unsigned)halves * 256 : 0);
-    const RowBuffers from(p, t);
+    const __amdgpu_buffer_rsrc_t qsr = row_buffer(p, t);
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_ptr_t)smem;
     constexpr unsigned kNone = 0xc0000000u;   // (and what a lane adds: past the end of weights and scales)
     // Rows past the tile's last read its first: what comes of them is not stored.
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4P
     const unsigned lane16 = lane * 16, lane4 = lane * 4;
     // load i of step s into the stage at `at`; past the last step nothing is read, so that the count of loads holds
     auto fetch = [&](int i, int s, unsigned at) {
-        load_to_lds(from.q, s < xsteps ? xvoff[i] + (unsigned)s * 128 : kPast, lds0 + at + (wave + i * T::kWaves) * 1024);
+        load_to_lds(qsr, s < xsteps ? xvoff[i] + (unsigned)s * 128 : kPast, lds0 + at + (wave + i * T::kWaves) * 1024);
     };
     i32x4 w[4][4], x[4];                 // weights of four halves; rows of four blocks
     unsigned ws[4], xs[2][T::kWords];    // their scales

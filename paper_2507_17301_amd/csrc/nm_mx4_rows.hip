@@ -130,13 +130,14 @@ __device__ inline double inverse_root(double a)
     return z == z ? z : y;
 }
 
-// NT threads a row, VPT units a thread, held in registers over the sum.  Loads go out in groups of units.
+// NT threads a row, VPT units a thread, held in registers over the sum.  Loads go out in groups of units: all of them, or as many as 1024 threads'
+// registers have room for (8192 x 16384 values, 512 x 4: 160 us, in twos 163, one by one 186).
 template <bool BF16, int NT, int VPT, bool SHORT>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void mx4_norm_kernel(Mx4Rows p)
 {
 #pragma clang fp contract(off)
     constexpr int ES = Elem<BF16>::kBytes, BLOCK = NT < 256 ? 256 : NT, RPB = BLOCK / NT;
-    constexpr int GROUP = VPT == 8 ? (NT < 1024 ? 4 : 1) : VPT == 4 && NT == 1024 ? 2 : VPT, AHEAD = VPT < 2 ? VPT : 2;   // AHEAD: units of gamma
+    constexpr int GROUP = VPT == 8 ? 1 : VPT == 4 && NT == 1024 ? 2 : VPT, AHEAD = VPT < 2 ? VPT : 2;   // AHEAD: units of gamma
     __shared__ double part[2][BLOCK / 64];   // in turn: a wavefront may still read one row's when another writes the next row's
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * RPB + (RPB > 1 ? threadIdx.x / NT : 0); row < p.rows; row += (int64_t)gridDim.x * RPB) {

@@ -56,6 +56,27 @@ def test_norm(width, dtype):
             assert h.dtype == TYPES[dtype] and torch.equal(h.cpu(), want_h.to(TYPES[dtype]))
 
 
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("width", [7, 8, 9, 4097, 4104, 5001, 8185, 8192, 8193, 12000, 16383, 16384])
+def test_norm_of_many_rows(width, dtype):
+    """Rows that fewer threads take than a few rows' would, the stream in place too."""
+    g = torch.Generator().manual_seed(width)
+    for rows, gap in ((256, 0), (261, 3)):
+        x, r = rows_of(g, rows, width, TYPES[dtype], gap), rows_of(g, rows, width, TYPES[dtype], gap)
+        gamma = 1.0 + 0.1 * torch.randn(width, generator=g)
+        say(f"rmsnorm_mx4 {rows} x {width} {dtype} gap {gap}")
+        v, want_h = norm_ref(x[:, :width], r[:, :width], gamma, 1e-6)
+        want, scales = round_ref(v)
+        xd, rd = on_gpu(x, width), on_gpu(r, width)
+        kept = x.cuda()[:, width:]
+        for out in (None, xd):
+            q, s, h = nm.nm_rmsnorm_mx4(xd, gamma.cuda(), rd, 1e-6, residual_out=out)
+            assert torch.equal(s.cpu().long(), scales) and same(values_of(q, s, width), want)
+            assert torch.equal(h.cpu(), want_h.to(TYPES[dtype]))
+        if gap:
+            assert torch.equal(torch.as_strided(xd, (rows, gap), (width + gap, 1), width), kept)
+
+
 def test_every_bf16_value():
     """All of them, the ties, the subnormals and those that are not finite, in blocks of nearly equal and of very different magnitudes."""
     bits = torch.arange(65536, dtype=torch.int32)
