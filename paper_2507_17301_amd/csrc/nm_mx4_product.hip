@@ -145,7 +145,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
 // of 256, each two halves of one matrix instruction's 128.
 // Rows go through LDS, NS steps of them, loaded straight into it: while a step is multiplied the next one's lie there and later ones' are on
 // their way; a wavefront reads the operand of 16 rows three before it is multiplied.
-// Weights go from memory into registers, SETS - 1 halves ahead: their layout in memory is the operands', and no other wavefront of the workgroup
+// Weights go from memory into registers, three halves ahead: their layout in memory is the operands', and no other wavefront of the workgroup
 // wants them.  Through LDS as well, LDS is what bounds the loop.
 // The rows' scales are dealt out in LDS for kSteps steps at once, as the lanes read them: a word has those of four blocks of 16 rows.
 // (Read byte by byte in the loop they made large products 3 to 8 % slower, dealt out by a kernel in front small ones 2 to 5 us.)
@@ -270,7 +270,7 @@ __device__ inline void store_tile4(const Mx4Product& p, const Channels4<GATED, 4
     }
 }
 
-template <int WR, int TB, int NS, int SETS, int PER_CU, bool GATED, int OUT>
+template <int WR, int TB, int NS, int PER_CU, bool GATED, int OUT>
 __global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4Product p, TileBands order)
 {
     using T = Tile4<WR, TB, NS>;
@@ -311,9 +311,8 @@ __global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4P
     auto fetch = [&](int i, int s, unsigned at) {
         load_to_lds(qsr, s < xsteps ? xvoff[i] + (unsigned)s * 128 : kPast, lds0 + at + (wave + i * T::kWaves) * 1024);
     };
-    constexpr int AHEAD = SETS - 1;
-    i32x4 w[SETS][4], x[4];              // weights of SETS halves; rows of four blocks
-    unsigned ws[SETS], xs[2][T::kWords];    // their scales
+    i32x4 w[4][4], x[4];                 // weights of four halves; rows of four blocks
+    unsigned ws[4], xs[2][T::kWords];    // their scales
     auto weights = [&](int set, int i, int half) {   // load i of a half's
         const unsigned at = half < halves ? (unsigned)half : kNone >> 12;
         if (i < 4) w[set][i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wsr, at * 4096 + i * 1024 + lane16, 0, 0));
@@ -380,7 +379,7 @@ __global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4P
         for (int i = 0; i < T::kXLoads; ++i) fetch(i, s, s * T::kXBytes);
     asm volatile("" : : : "memory");   // (rows first, so that the weights may still be out when they have landed)
 #pragma unroll
-    for (int s = 0; s < AHEAD; ++s)
+    for (int s = 0; s < 3; ++s)
 #pragma unroll
         for (int i = 0; i < 5; ++i) weights(s, i, s);
 #pragma unroll
@@ -390,7 +389,7 @@ __global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4P
     for (int j = 0; j < TB; ++j)
 #pragma unroll
         for (int b = 0; b < 4; ++b) acc[j][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(AHEAD * 5) : "memory");
+    asm volatile("s_waitcnt vmcnt(15) lgkmcnt(0)\n\ts_barrier" : : : "memory");
 #pragma unroll
     for (int j = 0; j < 3; ++j) rows(0, j, 0);
 #pragma unroll
@@ -429,22 +428,22 @@ __global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4P
 #pragma unroll
             for (int j = 0; j < TB; ++j) {
                 // In a step's second half, once all of its rows are read: all wavefronts have read this stage, and the next one has landed.  Younger
-                // than its loads are those of NS - 2 steps and of the weights of AHEAD halves at least.
+                // than its loads are those of NS - 2 steps and of the weights of three halves at least.
                 if (h == 1 && j == TB - 3)
-                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((NS - 2) * T::kXLoads + AHEAD * 5) : "memory");
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((NS - 2) * T::kXLoads + 15) : "memory");
                 if (j + 3 < TB) rows(h, j + 3, now);
                 else rows(1 - h, j + 3 - TB, h == 0 ? now : then);
                 if (j >= TB - 3 && j - (TB - 3) < T::kWords) words(1 - h, j - (TB - 3), scales + (q + 1) * T::kHalf);
                 if constexpr (TB == 4) {
-                    weights((q + AHEAD) % SETS, j, k + q + AHEAD);
-                    if (j == 3) weights((q + AHEAD) % SETS, 4, k + q + AHEAD);
+                    weights((q + 3) & 3, j, k + q + 3);
+                    if (j == 3) weights((q + 3) & 3, 4, k + q + 3);
                 } else {
-                    if (j < 5) weights((q + AHEAD) % SETS, j, k + q + AHEAD);
+                    if (j < 5) weights((q + 3) & 3, j, k + q + 3);
                 }
                 if (h == 1 && j >= TB - 3)
 #pragma unroll
                     for (int i = (j - TB + 3) * T::kXLoads / 3; i < (j - TB + 4) * T::kXLoads / 3; ++i) fetch(i, (k + q) / 2 + NS, now);
-                multiply(q % SETS, h, j);
+                multiply(q, h, j);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (h == 1) now = then;
@@ -594,16 +593,15 @@ struct Mx4Plan {
 };
 
 // The tile kernels' shapes.  More rows a workgroup read weights less often and keep the matrix units busier; fewer make more workgroups, and
-// leave less of a group's last tile empty.  Three workgroups a CU cover one another's start and end, but ask for weights one half step ahead only.
+// leave less of a group's last tile empty.
 struct Shape4 {
     int wr, rows, waves, per_cu;      // per_cu: workgroups that a CU holds (by registers)
-    float fixed, alone, shared;       // us: of a tile; of a step with one workgroup a CU, with all that a CU holds
+    float fixed, alone, shared;       // us: of a tile; of a step with one workgroup a CU, with two
 };
-constexpr Shape4 kShapes4[] = {{4, 128, 4, 2, 8.0f, 0.54f, 1.78f},    // 256 packed channels x 128 rows
-                               {4, 64, 4, 2, 4.7f, 0.54f, 1.16f},
-                               {4, 64, 4, 3, 6.0f, 0.85f, 1.62f}};
+constexpr Shape4 kShapes4[] = {{4, 128, 4, 2, 5.5f, 0.70f, 1.80f},    // 256 packed channels x 128 rows
+                               {4, 64, 4, 2, 5.0f, 0.49f, 1.15f}};
 
-template <int SHAPE, int TB, int NS, int SETS, bool GATED, int OUT>
+template <int SHAPE, int TB, int NS, bool GATED, int OUT>
 int launch_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 {
     constexpr int WR = kShapes4[SHAPE].wr, PER_CU = kShapes4[SHAPE].per_cu;
@@ -616,9 +614,9 @@ int launch_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
         return NM_ERR_SHAPE;
     }
     static unsigned long long done = 0;
-    const int rc = allow_lds((const void*)mx4_tile_kernel<WR, TB, NS, SETS, PER_CU, GATED, OUT>, T::kLds, &done);
+    const int rc = allow_lds((const void*)mx4_tile_kernel<WR, TB, NS, PER_CU, GATED, OUT>, T::kLds, &done);
     if (rc != NM_OK) return rc;
-    hipLaunchKernelGGL((mx4_tile_kernel<WR, TB, NS, SETS, PER_CU, GATED, OUT>), dim3((unsigned)grid), dim3(T::kWaves * 64), T::kLds, s, p, o);
+    hipLaunchKernelGGL((mx4_tile_kernel<WR, TB, NS, PER_CU, GATED, OUT>), dim3((unsigned)grid), dim3(T::kWaves * 64), T::kLds, s, p, o);
     NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }
@@ -626,9 +624,8 @@ int launch_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 template <bool GATED, int OUT>
 int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 {
-    if (pl.shape == 0) return launch_tile4<0, 8, 3, 4, GATED, OUT>(p, pl, s);
-    if (pl.shape == 1) return launch_tile4<1, 4, 4, 4, GATED, OUT>(p, pl, s);
-    return launch_tile4<2, 4, 4, 2, GATED, OUT>(p, pl, s);
+    if (pl.shape == 0) return launch_tile4<0, 8, 3, GATED, OUT>(p, pl, s);
+    return launch_tile4<1, 4, 4, GATED, OUT>(p, pl, s);
 }
 
 }  // namespace
@@ -639,10 +636,10 @@ int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 //   128 x 12288 -> 4096 17.9 and 46, 200 x 4096 -> 4096 11.0 and 12.9, 333 x 4096 -> 4096 17 and 13, 128 x 8192 -> 8192 17.9 and 32, 128 x 4096
 //   -> 10240 18.5 and 18.8, 32 x 4096 -> 65536 30 and 31, 48 rows 37 and 32, 64 x 4096 -> 32768 22 and 25; 64 experts, 2048 -> 2 x 1024, of 8 rows each
 //   28 and 32, 16 rows 34 and 32, 1024 -> 2048 15.8 and 15.7, 22 and 15.9; 60 experts, 1440 -> 1111, of 9 rows 13.9 and 15.4.
-// Of the tile kernels that with the least estimated time: rounds of workgroups over 256 CUs.  Of groups, which are uneven, five eighths of a tile each are
-// taken as empty, and half a round as the end of more than one.  us, 128 rows, 64 and 64 with three workgroups a CU: 512 x 4096 -> 4096 17.1, 13.3 and
-// 19.5, 2048 x 4096 -> 8192 36, 47 and 51, 8192 x 4096 -> 16384 260, 315 and 314; 64 experts, 2048 -> 2 x 1024, of 64 rows each 37, 32 and 35, 128 rows
-// 45, 42 and 39, 256 rows 62, 63 and 57, 512 rows 108, 119 and 117; 60 experts, 1440 -> 1111, of 200 rows 35, 33 and 32.
+// Of the tile kernels that with the least estimated time: rounds of workgroups over 256 CUs, two a CU; a group leaves five eighths of a tile empty (half,
+// but for those of fewer rows than a tile).
+// us, 128 rows and 64: 512 x 4096 -> 4096 17.4 and 13.3, 2048 x 4096 -> 8192 37 and 50, 8192 x 4096 -> 16384 270 and 330, 60 experts
+// of 12004 x 1440 -> 1111 35 and 35, 64 of 4096 x 2048 -> 2 x 1024 36 and 32, of 32768 103 and 120.
 // (One workgroup after another on a CU's slots, the next tile asked for before the last is stored: 0 to 16 % slower.)
 static Mx4Plan mx4_plan(const Mx4Product& p)
 {
@@ -657,12 +654,8 @@ static Mx4Plan mx4_plan(const Mx4Product& p)
         const Shape4& k = kShapes4[sh];
         const int64_t tall = !p.grouped ? (p.rows + k.rows - 1) / k.rows : p.rows / k.rows + (groups * (int64_t)5 + 7) / 8;
         const int64_t tiles = (tall < groups ? groups : tall) * ((p.groups + k.wr - 1) / k.wr);
-        const int64_t slots = 256 * k.per_cu, rounds = tiles / slots, rest = tiles % slots;
-        auto round = [&](int64_t n) {   // of n workgroups
-            const int64_t others = (n + 255) / 256 - 1;   // on a CU besides one
-            return k.fixed + p.steps * (k.alone + (k.shared - k.alone) * others / (k.per_cu - 1));
-        };
-        const float us = p.grouped && tiles > slots ? ((float)tiles / slots + 0.5f) * round(slots) : rounds * round(slots) + (rest ? round(rest) : 0.0f);
+        const int64_t rounds = tiles / 512, rest = tiles % 512;
+        const float us = rounds * (k.fixed + p.steps * k.shared) + (rest ? k.fixed + p.steps * (rest > 256 ? k.shared : k.alone) : 0.0f);
         if (us < least) {
             least = us;
             pl.shape = sh;
