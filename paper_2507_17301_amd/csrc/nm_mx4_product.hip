@@ -638,9 +638,12 @@ int pick_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
 //   28 and 32, 16 rows 34 and 32, 1024 -> 2048 15.8 and 15.7, 22 and 15.9; 60 experts, 1440 -> 1111, of 9 rows 13.9 and 15.4.
 // Of the tile kernels that with the least estimated time: rounds of workgroups over 256 CUs, two a CU; a group leaves five eighths of a tile empty (half,
 // but for those of fewer rows than a tile).
-// us, 128 rows and 64: 512 x 4096 -> 4096 17.4 and 13.3, 2048 x 4096 -> 8192 37 and 50, 8192 x 4096 -> 16384 270 and 330, 60 experts
-// of 12004 x 1440 -> 1111 35 and 35, 64 of 4096 x 2048 -> 2 x 1024 36 and 32, of 32768 103 and 120.
-// (One workgroup after another on a CU's slots, the next tile asked for before the last is stored: 0 to 16 % slower.)
+// us, 128 rows and 64, weights out of HBM: 512 x 4096 -> 4096 17.2 and 13.3, 2048 x 4096 -> 8192 39 and 55; 64 experts, 2048 -> 2 x 1024, of 64 rows each
+// 44 and 41, 128 rows 50 and 53, 256 rows 69 and 77, 512 rows 115 and 129; 256 experts, 2048 -> 2 x 512, of 32 rows 68 and 63; 60 experts, 1440 ->
+// 1111, of 200 rows 44 and 43.  8192 x 4096 -> 16384 270 and 330.
+// (Dropped: one workgroup after another on a CU's slots, the next tile asked for before the last is stored, 0 to 16 % slower; three workgroups of 64 rows a
+// CU, weights one half step ahead, 8 to 11 % faster at 128 to 256 rows of an expert whose weights lie in the last-level cache, 0 to 11 % slower
+// out of HBM.)
 static Mx4Plan mx4_plan(const Mx4Product& p)
 {
     Mx4Plan pl;
