@@ -733,7 +733,7 @@ def _mx4_rows(norm: bool, x, gamma, residual, eps, q, scales, residual_out):
     elif residual is not None:
         residual_out = _q8_like(x, dtype)
         optr = residual_out.data_ptr()
-    q, scales, ldq, lds = _mx4_out(x, x.shape[:-1], width, q, scales, dev)
+    q, scales, ldq, lds = _mx4_out(x, (rows,) if x.dim() == 2 else x.shape[:-1], width, q, scales, dev)
     rc = L.nm_rows_mx4_args(_ROWS4_ARGS.pack(x.data_ptr(), rptr, gptr, optr, q.data_ptr(), scales.data_ptr(), _q8_stream(dev), code, rows, width, ld,
                                              ldr, ldo, ldq, lds, norm, eps))
     if rc < 0:
@@ -771,7 +771,7 @@ def nm_dequantize_mx4(q, scales, width=None, dtype=None, y=None, stream=None):
         width = nb * 32 if y is None else y.shape[-1]
     if (width + 31) // 32 != nb:
         raise ValueError(f"rows of {nb} blocks do not hold {width} values")
-    shape, ldy = q.shape[:-1] + (width,), width
+    shape, ldy = (rows, width) if q.dim() == 2 else q.shape[:-1] + (width,), width
     if y is None:
         dtype = dtype or _torch.float32
         y = q.new_empty(shape, dtype=dtype)
@@ -851,7 +851,7 @@ def _mx4_product(q, scales, w: MX4Weights, offsets, index, bias, residual, dtype
         raise ValueError(f"rows of {nb} blocks, weights of {w.blocks}")
     optr = iptr = bptr = rptr = ldr = sptr = ldys = 0
     rows, outs = sources, w.outs
-    lead = q.shape[:-1]
+    lead = (sources,) if q.dim() == 2 else q.shape[:-1]
     if offsets is not None:
         optr = _int_vector(offsets, "offsets", w.experts + 1, dev)
         if index is not None:
