@@ -1,17 +1,20 @@
 // Routing of tokens to experts, and the weighted sum of what the experts answer.
 #include "nm_mx4_device.h"
 
+#include <type_traits>
+
 namespace nm {
 namespace {
 
 // ---------------------------------------------------------------- routing
 // Tokens go by in chunks, one a workgroup, a chunk in batches of 64.  A token belongs to L lanes, of V adjacent experts each.  A logit and its
-// expert are one double in [1, 2): 32 bits of the fraction sort like the logits, 10 below them fall with the expert, so that a maximum of
-// doubles finds the largest logit and of equal ones the lowest expert.  The choices are taken one after another.
+// expert are one number (a rank): its upper bits sort like the logits, 10 below them fall with the expert, so that a maximum finds the largest
+// logit and of equal ones the lowest expert.  Of bf16 it has 32 bits; of fp32 it is a double in [1, 2), with 42 bits of the fraction.
+// The choices are taken one after another.
 // The order by expert comes of one 64-bit mask an expert and batch, with a bit for each token that chose it: an expert's count is the number of
 // its bits, a token's place among the batch's the number of bits below its own.  So no order of atomics shows in a result.
 // Bound by the launches and the chain of steps for few tokens (16 x 64 logits 5.0 us), for many by the vector instructions of the choices (16384
-// x 256 in bf16, 8 choices: 11.4 us, 8 MB of logits; with key and expert compared apart 14.2) and by what the second kernel adds up.
+// x 256, 8 choices: 10.2 us in bf16, 11.9 in fp32; with key and expert compared apart 14.2) and by what the second kernel adds up.
 constexpr int kThreads = 1024, kBatch = NM_ROUTE_ONE_LAUNCH, kChunks = 256;
 static_assert(kBatch == 64, "a bit for each token");
 
@@ -23,59 +26,81 @@ template <int CTRL> __device__ inline double dpp(double v)
     return __builtin_bit_cast(double, (uint64_t)dpp<CTRL>((unsigned)(u >> 32)) << 32 | dpp<CTRL>((unsigned)u));
 }
 
-// fmax of doubles that are no NaN (the compiler makes its own of two instructions each)
-__device__ inline double larger(double a, double b)
-{
-    double r;
-    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-    return r;
-}
-
-template <int L> __device__ inline double best_of(double b)
-{
-    b = fmax(b, dpp<0xb1>(b));    // lane ^ 1
-    b = fmax(b, dpp<0x4e>(b));    // lane ^ 2
-    b = fmax(b, dpp<0x141>(b));   // mirrored in eight
-    b = fmax(b, dpp<0x140>(b));   // mirrored in sixteen
-    if constexpr (L == 64) {
-        b = fmax(b, __shfl_xor(b, 16));
-        b = fmax(b, __shfl_xor(b, 32));
-    }
-    return b;
-}
-
 template <int L> __device__ inline float sum_of(float v)
 {
     for (int m = 1; m < L; m <<= 1) v += __shfl_xor(v, m);
     return v;
 }
 
-constexpr unsigned kClosed = 0x007fffffu;   // the key of minus infinity; no open expert has one as small
-
-// 0 and -0 are the same, a NaN is more than infinity.
+// 32 bits that sort like the values.  0 and -0 are the same, a NaN is more than infinity.
 __device__ inline unsigned key_of(float f)
 {
     if (f != f) return 0xffffffffu;
     const unsigned u = __float_as_uint(f + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ inline double pack(unsigned key, int expert)
-{
-    return __builtin_bit_cast(double, 0x3ff0000000000000ull | (uint64_t)key << 10 | (unsigned)(NM_ROUTE_MAX_EXPERTS - 1 - expert));
-}
-__device__ inline unsigned key_in(double d) { return (unsigned)(__builtin_bit_cast(uint64_t, d) >> 10); }
-__device__ inline unsigned low_word(double d) { return (unsigned)__builtin_bit_cast(uint64_t, d); }   // tells experts apart
-__device__ inline double taken(double d) { return __builtin_bit_cast(double, 0x3ff0000000000000ull | low_word(d)); }   // (a key below 2^22: closed)
-__device__ inline int expert_in(double d) { return NM_ROUTE_MAX_EXPERTS - 1 - (int)(low_word(d) & (NM_ROUTE_MAX_EXPERTS - 1)); }
 __device__ inline float logit_of(unsigned key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+constexpr unsigned kClosed = 0x007fffffu;   // the key of minus infinity; no open expert has one as small
+constexpr int kLast = NM_ROUTE_MAX_EXPERTS - 1;
 
-// The packed logits of V adjacent experts of a token.
-template <int V> __device__ inline void logits_of(const Route& r, int64_t token, int first, double (&best)[V])
+template <bool BF16> struct Rank;
+template <> struct Rank<true> {   // (a key's lower 16 bits are those of its sign)
+    using Type = unsigned;
+    static __device__ inline Type make(float f, int expert) { return (key_of(f) >> 16) << 10 | (unsigned)(kLast - expert); }
+    static __device__ inline bool open(Type r) { return r >> 10 > kClosed >> 16; }
+    static __device__ inline float logit(Type r) { return logit_of((r >> 10) << 16 | (r >> 25 & 1 ? 0u : 0xffffu)); }
+    static __device__ inline int expert(Type r) { return kLast - (int)(r & kLast); }
+    static __device__ inline Type larger(Type a, Type b) { return max(a, b); }
+    template <int CTRL> static __device__ inline Type with(Type r) { return max(r, dpp<CTRL>(r)); }
+    static __device__ inline Type without(Type r, Type taken) { return r == taken ? 0u : r; }
+};
+template <> struct Rank<false> {
+    using Type = double;
+    static __device__ inline unsigned low(Type r) { return (unsigned)__builtin_bit_cast(uint64_t, r); }   // (tells experts apart)
+    static __device__ inline unsigned key(Type r) { return (unsigned)(__builtin_bit_cast(uint64_t, r) >> 10); }
+    static __device__ inline Type make(float f, int expert)
+    {
+        return __builtin_bit_cast(double, 0x3ff0000000000000ull | (uint64_t)key_of(f) << 10 | (unsigned)(kLast - expert));
+    }
+    static __device__ inline bool open(Type r) { return key(r) > kClosed; }
+    static __device__ inline float logit(Type r) { return logit_of(key(r)); }
+    static __device__ inline int expert(Type r) { return kLast - (int)(low(r) & kLast); }
+    // fmax of doubles that are no NaN (the compiler makes its own of two instructions each)
+    static __device__ inline Type larger(Type a, Type b)
+    {
+        Type r;
+        asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+        return r;
+    }
+    template <int CTRL> static __device__ inline Type with(Type r) { return fmax(r, dpp<CTRL>(r)); }
+    static __device__ inline Type without(Type r, Type taken)   // (leaves a key below 2^22: closed)
+    {
+        return low(r) == low(taken) ? __builtin_bit_cast(double, 0x3ff0000000000000ull | low(r)) : r;
+    }
+};
+
+template <int L, bool BF16> __device__ inline typename Rank<BF16>::Type best_of(typename Rank<BF16>::Type b)
 {
+    using R = Rank<BF16>;
+    b = R::template with<0xb1>(b);    // lane ^ 1
+    b = R::template with<0x4e>(b);    // lane ^ 2
+    b = R::template with<0x141>(b);   // mirrored in eight
+    b = R::template with<0x140>(b);   // mirrored in sixteen
+    if constexpr (L == 64) {
+        b = max(b, __shfl_xor(b, 16));
+        b = max(b, __shfl_xor(b, 32));
+    }
+    return b;
+}
+
+// The ranks of V adjacent experts of a token.
+template <int V, bool BF16> __device__ inline void ranks_of(const Route& r, int64_t token, int first, typename Rank<BF16>::Type (&rank)[V])
+{
+    constexpr int ES = Elem<BF16>::kBytes;
     float f[V];
-    const char* row = (const char*)r.logits + (token * r.ld + first) * (r.bf16 ? 2 : 4);
+    const char* row = (const char*)r.logits + (token * r.ld + first) * ES;
     if (first + V <= r.experts) {   // (through memcpy: rows start anywhere)
-        if (r.bf16) {
+        if constexpr (BF16) {
             unsigned w[V / 2];
             __builtin_memcpy(w, row, V * 2);
 #pragma unroll
@@ -85,56 +110,54 @@ template <int V> __device__ inline void logits_of(const Route& r, int64_t token,
         }
     } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            f[v] = -__builtin_inff();
-            if (first + v < r.experts) f[v] = r.bf16 ? Elem<true>::load1(row + v * 2) : Elem<false>::load1(row + v * 4);
-        }
+        for (int v = 0; v < V; ++v) f[v] = first + v < r.experts ? Elem<BF16>::load1(row + v * ES) : -__builtin_inff();
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) best[v] = pack(key_of(f[v]), first + v);
+    for (int v = 0; v < V; ++v) rank[v] = Rank<BF16>::make(f[v], first + v);
 }
 
 // Chooses for the tokens of one batch; their bits go into mask.
-template <int L, int V>
+template <int L, int V, bool BF16>
 __device__ inline void choose(const Route& r, int64_t first, int count, unsigned long long* mask)
 {
     constexpr int PER = kThreads / L, SLOTS = NM_ROUTE_MAX_CHOICES / L;   // tokens at a time; choices a lane keeps
     const int l = threadIdx.x % L;
     for (int t = threadIdx.x / L; t < count; t += PER) {
         const int64_t token = first + t;
-        double best[V];
-        logits_of<V>(r, token, l * V, best);
+        using R = Rank<BF16>;
+        typename R::Type rank[V];
+        ranks_of<V, BF16>(r, token, l * V, rank);
         float top = 0.0f, sum = 0.0f, p[SLOTS];
         int id[SLOTS];
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) { p[s] = 0.0f; id[s] = -1; }
         for (int j = 0; j < r.choices; ++j) {
-            double half = best[V / 2], b = best[0];
+            typename R::Type half = rank[V / 2], b = rank[0];
 #pragma unroll
             for (int v = 1; v < V / 2; ++v) {
-                b = larger(b, best[v]);
-                half = larger(half, best[V / 2 + v]);
+                b = R::larger(b, rank[v]);
+                half = R::larger(half, rank[V / 2 + v]);
             }
-            b = best_of<L>(fmax(b, half));
-            if (key_in(b) <= kClosed) break;   // (the same for all lanes of a token)
-            const float logit = logit_of(key_in(b));
+            b = best_of<L, BF16>(max(b, half));
+            if (!R::open(b)) break;   // (the same for all lanes of a token)
+            const float logit = R::logit(b);
             if (j == 0) {
                 top = logit;
                 if (!r.normalise) {
                     float part = 0.0f;
 #pragma unroll
                     for (int v = 0; v < V; ++v)
-                        if (key_in(best[v]) > kClosed) part += expf(logit_of(key_in(best[v])) - top);
+                        if (R::open(rank[v])) part += expf(R::logit(rank[v]) - top);
                     sum = sum_of<L>(part);
                 }
             }
 #pragma unroll
-            for (int v = 0; v < V; ++v) best[v] = low_word(best[v]) == low_word(b) ? taken(best[v]) : best[v];
+            for (int v = 0; v < V; ++v) rank[v] = R::without(rank[v], b);
             const float e = expf(logit - top);
             if (r.normalise) sum += e;
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s)
-                if (j == s * L + l) { p[s] = e; id[s] = expert_in(b); }
+                if (j == s * L + l) { p[s] = e; id[s] = R::expert(b); }
         }
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
@@ -204,7 +227,7 @@ __device__ inline int scan(Shared& s, int experts)
 __host__ __device__ inline int count_stride(int experts) { return (experts + 3) & ~3; }
 
 // All that there is to do where the tokens are one batch; otherwise the choices and each chunk's counts.
-template <int L, int V>
+template <int L, int V, bool BF16>
 __global__ __launch_bounds__(kThreads) void route_choose_kernel(Route r, int chunk, void* counts)
 {
     __shared__ Shared s;
@@ -216,7 +239,7 @@ __global__ __launch_bounds__(kThreads) void route_choose_kernel(Route r, int chu
         if (e < r.experts) s.mask[e] = 0;
         __syncthreads();
         const int count = (int)(end - at < kBatch ? (end > at ? end - at : 0) : kBatch);
-        choose<L, V>(r, at, count, s.mask);
+        choose<L, V, BF16>(r, at, count, s.mask);
         __syncthreads();
         if (e < r.experts) total += __popcll(s.mask[e]);
     }
@@ -381,9 +404,14 @@ int run_route(const Route& r, void* workspace, hipStream_t s)
     const int chunk = one ? kBatch : chunk_of(r.tokens);
     const dim3 grid(one ? 1u : (unsigned)((r.tokens + chunk - 1) / chunk));
     void* counts = one ? nullptr : workspace;
-    if (r.experts <= 64) hipLaunchKernelGGL((route_choose_kernel<16, 4>), grid, dim3(kThreads), 0, s, r, chunk, counts);
-    else if (r.experts <= 256) hipLaunchKernelGGL((route_choose_kernel<16, 16>), grid, dim3(kThreads), 0, s, r, chunk, counts);
-    else hipLaunchKernelGGL((route_choose_kernel<64, 16>), grid, dim3(kThreads), 0, s, r, chunk, counts);
+    auto choose = [&](auto bf16) {
+        constexpr bool BF16 = decltype(bf16)::value;
+        if (r.experts <= 64) hipLaunchKernelGGL((route_choose_kernel<16, 4, BF16>), grid, dim3(kThreads), 0, s, r, chunk, counts);
+        else if (r.experts <= 256) hipLaunchKernelGGL((route_choose_kernel<16, 16, BF16>), grid, dim3(kThreads), 0, s, r, chunk, counts);
+        else hipLaunchKernelGGL((route_choose_kernel<64, 16, BF16>), grid, dim3(kThreads), 0, s, r, chunk, counts);
+    };
+    if (r.bf16) choose(std::true_type{});
+    else choose(std::false_type{});
     NM_HIP_CHECK(hipGetLastError());
     if (one) return NM_OK;
     if (chunk == kBatch) hipLaunchKernelGGL((route_place_kernel<true>), grid, dim3(kThreads), 0, s, r, chunk, (const void*)counts);
