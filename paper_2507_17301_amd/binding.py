@@ -935,15 +935,18 @@ def nm_route(logits, k: int, normalise: bool = True, stream=None) -> Routing:
     dev, i32 = logits.get_device(), _torch.int32
     ids, weights, slots = logits.new_empty((3,) + logits.shape[:-1] + (k,), dtype=i32).unbind()   # (one allocation instead of three)
     weights = weights.view(_torch.float32)
-    offsets, rows = logits.new_empty(experts + 1 + tokens * k, dtype=i32).split_with_sizes((experts + 1, tokens * k))
-    nbytes, ws = 0, None
-    if tokens > NM_ROUTE_ONE_LAUNCH:   # (else none is needed)
+    nbytes = wptr = 0
+    if tokens > NM_ROUTE_ONE_LAUNCH:   # (else no workspace is needed)
         need = ctypes.c_size_t(0)
         _check(L.nm_route_workspace(tokens, experts, ctypes.byref(need)))
         nbytes = need.value
-        ws = logits.new_empty(nbytes, dtype=_torch.uint8)
+        words = (nbytes + 15) // 16 * 4
+        ws, offsets, rows = logits.new_empty(words + experts + 1 + tokens * k, dtype=i32).split_with_sizes((words, experts + 1, tokens * k))
+        wptr = ws.data_ptr()
+    else:
+        offsets, rows = logits.new_empty(experts + 1 + tokens * k, dtype=i32).split_with_sizes((experts + 1, tokens * k))
     rc = L.nm_route_args(_ROUTE_ARGS.pack(logits.data_ptr(), ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(),
-                                          0 if ws is None else ws.data_ptr(), _q8_stream(dev), _q8_code(logits.dtype, "logits"), tokens, experts, ld, k,
+                                          wptr, _q8_stream(dev), _q8_code(logits.dtype, "logits"), tokens, experts, ld, k,
                                           bool(normalise), nbytes))
     if rc < 0:
         _check(rc)
