@@ -65,29 +65,34 @@ class FeedForwardMX4:
 class ExpertsMX4:
     """A layer of experts: up: gated weights of each (2 * hidden channels of `width`), down: `width` channels of `hidden`;
     every token goes through the k experts with its largest logits, whose answers are weighted with their softmax.
+    answers: the type in which an expert's answer goes to that sum.  fp32 (the default): only the sum is rounded, to x's type.  bf16
+    halves the answers' bytes and rounds each of them, by 2^-8 of itself at most.
     from_float() makes the weights from fp32 or bf16 tensors."""
 
-    def __init__(self, up: nm.MX4Weights, down: nm.MX4Weights, k: int, normalise: bool = True):
+    def __init__(self, up: nm.MX4Weights, down: nm.MX4Weights, k: int, normalise: bool = True, answers=None):
+        import torch
         _check_pair(up, down)
         if up.experts != down.experts or not 1 <= k <= up.experts:
             raise ValueError(f"up has {up.experts} experts, down {down.experts}; {k} are chosen")
-        self.up, self.down, self.k, self.normalise = up, down, k, normalise
+        if answers not in (None, torch.float32, torch.bfloat16):
+            raise ValueError(f"answers are fp32 or bf16, not {answers}")
+        self.up, self.down, self.k, self.normalise, self.answers = up, down, k, normalise, answers or torch.float32
 
     @classmethod
-    def from_float(cls, gate_w, up_w, down_w, k: int, normalise: bool = True):
+    def from_float(cls, gate_w, up_w, down_w, k: int, normalise: bool = True, answers=None):
         """gate_w, up_w [experts, hidden, width], down_w [experts, width, hidden] on the device, fp32 or bf16."""
         import torch
-        return cls(nm.nm_mx4_pack(torch.cat([gate_w, up_w], dim=1), gated=True), nm.nm_mx4_pack(down_w), k, normalise)
+        return cls(nm.nm_mx4_pack(torch.cat([gate_w, up_w], dim=1), gated=True), nm.nm_mx4_pack(down_w), k, normalise, answers)
 
     def forward(self, x, logits, residual=None, stream=None):
         """x, residual: [..., width] in bf16 or fp32 (x: the normalised rows); logits [..., experts].  Returns residual plus the
-        experts' answers, shaped and typed like x.  The answers that are summed are bf16 for bf16 rows, fp32 for fp32."""
+        experts' answers, shaped and typed like x."""
         if x.shape[:-1] != logits.shape[:-1] or logits.shape[-1] != self.up.experts:
             raise ValueError(f"rows {tuple(x.shape)} and logits {tuple(logits.shape)} for {self.up.experts} experts do not fit together")
         to = nm.nm_route(logits, self.k, self.normalise, stream=stream)
         q, s = nm.nm_quantize_mx4(x, stream=stream)
         q, s = nm.nm_experts_mx4(q, s, self.up, to.offsets, to.rows, rounded=True, stream=stream)
-        y = nm.nm_experts_mx4(q, s, self.down, to.offsets, dtype=x.dtype, stream=stream)
+        y = nm.nm_experts_mx4(q, s, self.down, to.offsets, dtype=self.answers, stream=stream)
         return nm.nm_combine(y, to.slots, to.weights, residual, dtype=x.dtype, stream=stream)
 
     __call__ = forward
