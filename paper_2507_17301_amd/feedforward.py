@@ -87,6 +87,8 @@ class ExpertsMX4:
     def forward(self, x, logits, residual=None, stream=None):
         """x, residual: [..., width] in bf16 or fp32 (x: the normalised rows); logits [..., experts].  Returns residual plus the
         experts' answers, shaped and typed like x."""
+        if x.shape[-1] != self.up.width:   # (blocks of 32 alone would let other widths pass)
+            raise ValueError(f"rows of {x.shape[-1]} values for experts of {self.up.width}")
         if x.shape[:-1] != logits.shape[:-1] or logits.shape[-1] != self.up.experts:
             raise ValueError(f"rows {tuple(x.shape)} and logits {tuple(logits.shape)} for {self.up.experts} experts do not fit together")
         to = nm.nm_route(logits, self.k, self.normalise, stream=stream)
