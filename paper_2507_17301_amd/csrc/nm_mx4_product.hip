@@ -24,12 +24,12 @@ template <int TB, int RB, int NW> constexpr int few4_lds()
 }
 
 template <int TB, int RB, int NW>
-__global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int parts)
+__global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int parts, int tile0)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int tile = blockIdx.x / parts, b0 = (blockIdx.x - tile * parts) * RB;   // (RB divides 4: a workgroup stays within its row group)
-    const RowTile t = GroupTiles(p, 16 * TB).at(p, tile);
+    const int in = blockIdx.x / parts, b0 = (blockIdx.x - in * parts) * RB;   // (RB divides 4: a workgroup stays within its row group)
+    const RowTile t = GroupTiles(p, 16 * TB).at(p, tile0 + in);
     if (t.count == 0) return;
     const size_t group = (size_t)t.expert * p.groups + (b0 >> 2);
     const __amdgpu_buffer_rsrc_t wsr = q8_rsrc(p.w + group * p.steps * 8192, (unsigned)p.steps * 8192);
@@ -271,16 +271,17 @@ __device__ inline void store_tile4(const Mx4Product& p, const Channels4<GATED, 4
 }
 
 template <int WR, int TB, int NS, int PER_CU, bool GATED, int OUT>
-__global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4Product p, TileBands order)
+__global__ __launch_bounds__(WR * 64, PER_CU * WR / 4) void mx4_tile_kernel(Mx4Product p, TileBands order, int block0)
 {
     using T = Tile4<WR, TB, NS>;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = scalar(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const GroupTiles groups(p, T::kRows);
     order.tiles_r = groups.all;   // (of experts, those that there are, so that they are dealt to all XCDs)
-    if ((int)blockIdx.x >= order.tiles()) return;
+    const int block = block0 + blockIdx.x;
+    if (block >= order.tiles()) return;
     int tc, tr;
-    order.at(blockIdx.x, tc, tr);
+    order.at(block, tc, tr);
     tc = scalar(tc);
     tr = scalar(tr);
     const RowTile t = groups.at(p, tr);
@@ -534,6 +535,9 @@ inline int64_t tiles_of(const Mx4Product& p, int per)
     return p.rows / per + (p.experts < p.rows ? p.experts : p.rows);
 }
 
+// Work-items of a launch.  A call that wants more is several launches.
+constexpr int64_t kMaxItems = 0xffffffffll;
+
 template <int TB, int RB, int NW>
 int launch_few4(const Mx4Product& p, hipStream_t s)
 {
@@ -543,14 +547,13 @@ int launch_few4(const Mx4Product& p, hipStream_t s)
         const int rc = allow_lds((const void*)mx4_few_kernel<TB, RB, NW>, LDS, &done);
         if (rc != NM_OK) return rc;
     }
-    const int parts = p.groups * 4 / RB;
-    const int64_t grid = tiles_of(p, 16 * TB) * parts;
-    if (grid > 0x7fffffff) {
-        set_error("%lld workgroups: too many", (long long)grid);
-        return NM_ERR_SHAPE;
+    const int parts = p.groups * 4 / RB;   // (at most 2^20, of channels up to 2^24)
+    const int64_t tiles = tiles_of(p, 16 * TB), each = kMaxItems / (NW * 64) / parts;
+    for (int64_t at = 0; at < tiles; at += each) {
+        const int64_t n = tiles - at < each ? tiles - at : each;
+        hipLaunchKernelGGL((mx4_few_kernel<TB, RB, NW>), dim3((unsigned)(n * parts)), dim3(NW * 64), LDS, s, p, parts, (int)at);
+        NM_HIP_CHECK(hipGetLastError());
     }
-    hipLaunchKernelGGL((mx4_few_kernel<TB, RB, NW>), dim3((unsigned)grid), dim3(NW * 64), LDS, s, p, parts);
-    NM_HIP_CHECK(hipGetLastError());
     return NM_OK;
 }
 
@@ -616,8 +619,12 @@ int launch_tile4(const Mx4Product& p, const Mx4Plan& pl, hipStream_t s)
     static unsigned long long done = 0;
     const int rc = allow_lds((const void*)mx4_tile_kernel<WR, TB, NS, PER_CU, GATED, OUT>, T::kLds, &done);
     if (rc != NM_OK) return rc;
-    hipLaunchKernelGGL((mx4_tile_kernel<WR, TB, NS, PER_CU, GATED, OUT>), dim3((unsigned)grid), dim3(T::kWaves * 64), T::kLds, s, p, o);
-    NM_HIP_CHECK(hipGetLastError());
+    constexpr int64_t kEach = kMaxItems / T::kThreads & ~7;   // (a multiple of the XCDs')
+    for (int64_t at = 0; at < grid; at += kEach) {
+        const unsigned n = (unsigned)(grid - at < kEach ? grid - at : kEach);
+        hipLaunchKernelGGL((mx4_tile_kernel<WR, TB, NS, PER_CU, GATED, OUT>), dim3(n), dim3(T::kThreads), T::kLds, s, p, o, (int)at);
+        NM_HIP_CHECK(hipGetLastError());
+    }
     return NM_OK;
 }
 
