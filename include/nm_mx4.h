@@ -88,7 +88,8 @@ int nm_mx4_export(const nm_mx4_t* w, uint8_t* q_host, uint8_t* scales_host);
  * nm_linear_mx4 -- rows in MX4 times weights in MX4:
  *   z_rc = sum_k x_rk * w_ck + bias_c            products exact, sums in fp32
  *   y_rc = z_rc + residual_rc                    plain weights
- *   y_rc = z_rc / (1 + exp(-z_rc)) * z_r,(c+C)   gated weights of 2 C channels (no residual)
+ *   y_rc = z_rc / (1 + exp(-z_rc)) * z_r,(c+C)   gated weights of 2 C channels (no residual), of the sums z within (2 |z_rc| + 12) 2^-24 of
+ *                                                itself, whatever y's type; 0 for gates z_rc below -174
  * rounded once to y_dtype: NM_F32, NM_BF16 (nearest even) or NM_MX4 (as by nm_quantize_mx4 of the fp32 values; no residual).
  * Calls with the same arguments give the same bits.  A row with a NaN gives a row of NaN and touches no other.
  *   q_dev, ldq, scales_dev, lds    rows of the weights' width
