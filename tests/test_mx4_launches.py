@@ -1,6 +1,7 @@
-"""What products in MX4 launch: every tile once, in launches that the GPU takes."""
+"""What products in MX4 launch: every tile once, in launches that the GPU takes; the kernels that the GPU tests' sizes are meant for."""
 import pytest
 
+import mx4_cases as cases
 from mx4_launches import BF16, F32, MX4, build, launches
 
 
@@ -44,3 +45,35 @@ def test_calls_of_ordinary_size_are_one_launch(ask):
     for got in ask(SIZES[:5]):
         assert len(got) == 1 and got[0].first == 0
     assert all(len(got) > 1 for got in ask([SIZES[7], SIZES[8], SIZES[10], SIZES[11]]))
+
+
+def _tiles(ask, sizes):
+    """Rows of the tiles that each size's one launch has, all of them tile kernels."""
+    out = []
+    for size, got in zip(sizes, ask(sizes)):
+        assert len(got) == 1 and got[0].name == "mx4_tile_kernel", (size, got)
+        out.append(got[0].rows)
+    return out
+
+
+@pytest.mark.parametrize("shape", sorted(cases.TILE_ROWS))
+def test_grouped_sizes_take_their_tiles(ask, shape):
+    for experts, entries, k, n in cases.GROUPED[shape] + [cases.GROUPED_LONG[shape]]:
+        for gated in (0, 1):
+            assert set(_tiles(ask, [(entries, experts, n, k, gated, out) for out in (F32, BF16, MX4)])) == {cases.TILE_ROWS[shape]}
+    rows, k, n = cases.LONG[shape]
+    assert _tiles(ask, [(rows, 0, n, k, gated, F32) for gated in (0, 1)]) == [cases.TILE_ROWS[shape]] * 2
+    # (24 steps' scales lie in LDS)
+    assert all((k + 255) // 256 > 24 for k in (k, cases.GROUPED_LONG[shape][2]))
+
+
+def test_other_sizes_take_tiles(ask):
+    rows, k, n = cases.FAR["rows"]
+    experts, entries, k2, n2 = cases.FAR["entries"]
+    experts3, entries3, _, k3, n3 = cases.FAR["index"]
+    experts4, entries4, k4, n4 = cases.HEAVY
+    _tiles(ask, [(rows, 0, n, k, 0, BF16), (entries, experts, n2, k2, 0, BF16), (entries3, experts3, n3, k3, 0, BF16), (entries4, experts4, n4, k4, 0, F32)])
+    for experts, choices, tokens, width, hidden in cases.EXPERTS_LAYERS:
+        _tiles(ask, [(tokens * choices, experts, 2 * hidden, width, 1, MX4), (tokens * choices, experts, width, hidden, 0, F32)])
+    for rows, width, hidden in cases.FEEDFORWARD:
+        _tiles(ask, [(rows, 0, 2 * hidden, width, 1, MX4), (rows, 0, width, hidden, 0, BF16)])
