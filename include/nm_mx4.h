@@ -49,8 +49,8 @@ int nm_dequantize_mx4(const uint8_t* q_dev, int64_t ldq, const uint8_t* scales_d
  *   n = 1 / sqrt(mean_i(h_i^2) + eps)            the mean and the root in 64 bits, n rounded to fp32
  *   v_i = (h_i * n) * gamma_i                    fp32, two roundings
  *   q, scales = v as by nm_quantize_mx4;  residual_out = h rounded to x_dtype
- * A power of two decides about a whole block, so n is held in 64 bits until the end: the codes are those of the formula, not those of
- * one order of summation.  A row for which n is not finite (a zero row with eps = 0) becomes NaN.
+ * A power of two decides about a whole block, so the sum and n are held in 64 bits until the end: another order of summation then
+ * gives another n, and with it perhaps other codes, in some rows of 10^8 (in 32 bits it would in most).  A row for which n is not finite (a zero row with eps = 0) becomes NaN.
  *   gamma_dev         fp32 [width], or NULL for 1;  eps finite, >= 0
  *   residual_out_dev  rows of x_dtype at stride ldo >= width, or NULL.  It may be x_dev or residual_dev itself (same stride).
  */
@@ -108,8 +108,9 @@ int nm_linear_mx4(const uint8_t* q_dev, int64_t ldq, const uint8_t* scales_dev, 
  * nm_linear_mx4 with expert e's weights and bias, of row r of x, or of row index[r] where an index is given.
  *   offsets_dev     int32 [experts + 1] on the device, not falling, from 0 to at most `entries` (as nm_route writes them).
  *                   Groups may be empty.  Values outside [0, entries] count as the nearer end, a group that ends before
- *                   it begins as empty.  Rows of y in no group are left as they were; where offsets fall, a row in
- *                   several groups holds what one of them gives or is left, too.
+ *                   it begins as empty.  Rows of y in no group are left as they were.  Where offsets fall, groups
+ *                   overlap, and what y's rows in any group hold is not defined: parts of one group's answer and of
+ *                   another's, or what was there.  Nothing else is written.
  *   index_dev       int32 [entries], or NULL.  An index outside [0, rows) makes its row of y NaN.
  *   entries         rows of y (without an index: also of x, rows = entries)
  *   bias_dev        fp32 [experts][channels], or NULL

@@ -131,6 +131,29 @@ def test_offsets_out_of_range(shape):
     assert (run([0] * 5) == 5).all() and (run([entries] * 5) == 5).all() and (run([2 ** 31 - 1] * 5) == 5).all() and (run([entries, 0, 0, 0, 0]) == 5).all()
 
 
+@pytest.mark.parametrize("entries", [1000, 8000])
+def test_offsets_that_fall(entries):
+    """Groups overlap, and may have more tiles than groups side by side could: a value is one group's or is left, and nothing else is written."""
+    experts, k, n = 5, 300, 1030
+    g = torch.Generator().manual_seed(entries)
+    h = nm.nm_mx4_pack(*(v.cuda() for v in random_mx4(g, (experts, n, k), 110, 122)), k)
+    q, s = (v.cuda() for v in random_mx4(g, (entries, k)))
+    say(f"experts_mx4 {entries} entries, offsets that fall")
+
+    def run(offsets):
+        y = torch.full((entries + 2, n + 2), 5.0, device="cuda")
+        nm.nm_experts_mx4(q, s, h, torch.tensor(offsets, dtype=torch.int32, device="cuda"), y=y[1:1 + entries, 1:1 + n])
+        return y
+    alone = [run([0] * (e + 1) + [entries] * (experts - e)) for e in range(experts)]   # all rows by expert e
+    for offsets in ([0, entries * 9 // 10, entries // 10, entries, 0, entries], [entries, 0, entries - 2, 0, entries - 1, 3]):
+        y = run(offsets)
+        fits = y == 5
+        for e in range(experts):
+            begin, end = 1 + offsets[e], 1 + max(offsets[e], offsets[e + 1])
+            fits[begin:end] |= y[begin:end] == alone[e][begin:end]
+        assert bool(fits.all())
+
+
 @pytest.mark.parametrize("shape", sorted(cases.GROUPED))
 def test_rows_in_no_group_are_left_as_they_were(shape):
     experts, entries, k, n = cases.GROUPED[shape][0]
