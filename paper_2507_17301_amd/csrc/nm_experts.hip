@@ -339,7 +339,8 @@ inline int chunk_of(int64_t tokens)
 }
 
 // ---------------------------------------------------------------- combination
-// Eight adjacent values of a row a thread.  Bound by HBM: the experts' rows are read once (4096 x 8 choices x 2048 in bf16: 33 us, 5.1 TB/s).
+// Eight adjacent values of a row a thread.  Bound by HBM: the experts' rows are read once (4096 x 8 choices x 2048: of fp32
+// 58 us, of bf16 31, 5.2 and 5.4 TB/s).
 template <bool YBF16, bool BF16>
 __global__ __launch_bounds__(256) void combine_kernel(Combine p, int units)
 {

@@ -6,7 +6,7 @@
 // (measured against 64 bits: within 2^-23 of the sum of the products' magnitudes).  Weights are its first operand, rows of x the second: lane l of
 // a wavefront then holds packed weight rows 4 (l / 16) .. + 3 of a 16-row block for row l % 16 of x, and the packing deals channels so that
 // the four blocks of a 64-row group give it twice 8 adjacent channels (gated: 8 adjacent outputs, gate and value in the same registers).
-// (Out of registers, on normally distributed values, this form does 7.0 PFLOP/s and the 32x32x64 one 6.3; on zeros 9.7 and 8.9.)
+// (Out of registers, on normally distributed values, this form does 7.0 to 7.3 PFLOP/s and the 32x32x64 one 6.2; on zeros 9.7 and 8.9.)
 #include "nm_mx4_product.h"
 
 namespace nm {
@@ -149,8 +149,10 @@ __global__ __launch_bounds__(NW * 64) void mx4_few_kernel(Mx4Product p, int part
 // wants them.  Through LDS as well, LDS is what bounds the loop.
 // The rows' scales are dealt out in LDS for kSteps steps at once, as the lanes read them: a word has those of four blocks of 16 rows.
 // (Read byte by byte in the loop they made large products 3 to 8 % slower, dealt out by a kernel in front small ones 2 to 5 us.)
-// Bound by power where all of the chip multiplies (8192 x 4096 -> 16384 240 to 300 us by the card, 3.7 to 4.6 PFLOP/s), by a tile's start and end where
-// K is short: of the 18.5 us of a tile of eight steps, gated and rounded, the loop takes 8.6, silu, rounding and stores 4.4, the first loads 2.7.
+// Where all of the chip multiplies the matrix units work 61 % of the cycles, at a clock that power decides (8192 x 4096 -> 16384 249 us at 1.7 GHz on
+// normally distributed values, 182 at 2.2 on zeros, as many cycles; the instruction alone 1.34 times as fast on zeros; by the card 240 to 300).
+// Where K is short a tile's start and end decide: of the 18.9 us of a tile of eight steps, gated and rounded, the loop takes 8.5, silu, rounding and
+// stores 5.0, the first loads 2.75.
 // A row's 128 bytes are 8 blocks of 16, block c stored at c ^ (row & 7), so that what an LDS cycle reads lies in different banks.
 template <int WR, int TB, int NS> struct Tile4 {
     static constexpr int kWaves = WR, kThreads = 64 * kWaves, kRows = 16 * TB;
