@@ -50,7 +50,8 @@ int nm_dequantize_mx4(const uint8_t* q_dev, int64_t ldq, const uint8_t* scales_d
  *   v_i = (h_i * n) * gamma_i                    fp32, two roundings
  *   q, scales = v as by nm_quantize_mx4;  residual_out = h rounded to x_dtype
  * A power of two decides about a whole block, so the sum and n are held in 64 bits until the end: another order of summation then
- * gives another n, and with it perhaps other codes, in some rows of 10^8 (in 32 bits it would in most).  A row for which n is not finite (a zero row with eps = 0) becomes NaN.
+ * gives another n, and with it perhaps other codes, in some rows of 10^8 (in 32 bits it would in most).  A row for which n is not
+ * finite (a zero row with eps = 0) becomes NaN.
  *   gamma_dev         fp32 [width], or NULL for 1;  eps finite, >= 0
  *   residual_out_dev  rows of x_dtype at stride ldo >= width, or NULL.  It may be x_dev or residual_dev itself (same stride).
  */
@@ -89,7 +90,7 @@ int nm_mx4_export(const nm_mx4_t* w, uint8_t* q_host, uint8_t* scales_host);
  *   z_rc = sum_k x_rk * w_ck + bias_c            products exact, sums in fp32
  *   y_rc = z_rc + residual_rc                    plain weights
  *   y_rc = z_rc / (1 + exp(-z_rc)) * z_r,(c+C)   gated weights of 2 C channels (no residual), of the sums z within (2 |z_rc| + 12) 2^-24 of
- *                                                itself, whatever y's type; 0 for gates z_rc below -174
+ *                                                itself (or 2^-148) before it is rounded to y's type; 0 for gates below -174.7
  * rounded once to y_dtype: NM_F32, NM_BF16 (nearest even) or NM_MX4 (as by nm_quantize_mx4 of the fp32 values; no residual).
  * Calls with the same arguments give the same bits.  A row with a NaN gives a row of NaN and touches no other.
  *   q_dev, ldq, scales_dev, lds    rows of the weights' width

@@ -147,7 +147,7 @@ template <bool GATED, int NB> struct Channels4 {
 
 // silu(gate) * up, with s = exp(-|gate| / 2): gate / (1 + s^2) for gates that are not negative, otherwise gate s / (1 + s^2) times s up.  Nothing
 // on the way leaves fp32's range before the result does, down to gates of -174 (s^2 as one number would at -87, and the reciprocal of
-// 1 + exp(-gate) is 0 there).  Below s is 0, and so is the result.
+// 1 + exp(-gate) is 0 there).  Under -174.7 s is 0, and so is the result.
 // u = 2^-24: s is within (|gate| + 2) u (its argument's constant and rounding, then 2 u of the instruction), the reciprocal within 2 u, the
 // sum and the four products round once each, and s counts twice at most: (2 |gate| + 12) u in all.  The gate itself is a sum of 128
 // products and more in fp32, of whose roundings silu takes over |gate| times as much: a quotient to the last bit would not show.
